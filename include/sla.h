@@ -406,6 +406,112 @@ int sla_gate_logits_backward(const sla_params* p, const void* x, const float* w,
                              float* dw, void* workspace, size_t workspace_bytes, void* stream);
 size_t sla_gate_logits_backward_workspace_bytes(const sla_params* p);
 
+/*
+ * What stands around the mixer inside a layer: rotary positions on the queries and keys in front of it, the normalised
+ * and gated read-out behind it, and the join with the residual stream.  Conventions as above (device pointers, nothing
+ * allocated, kept or synchronised, a status code, on error nothing launched); tensors 16-byte aligned, int32 arrays 4-byte,
+ * frequencies 8-byte.  Packed batches: with cu_seqlens [B+1] int32 (device) the tensors are those of one batch row of T
+ * tokens in all, and tokens outside every sequence are neither read nor written nor counted in a sum (offsets are clamped as for
+ * sla_forward_varlen); cu_seqlens NULL: rectangular [B,T,...].  One token of each of B sequences is T = 1.
+ *
+ * Rotary positions.  The first `rotary` elements of every head vector are pairs (a, b), turned by the angle
+ * th = position * frequency and scaled:
+ *     a' = m (a cos th - b sin th),   b' = m (a sin th + b cos th);      elements from `rotary` on are copied.
+ * Pair i is elements (i, i + rotary/2), or with SLA_FLAG_ADJACENT_PAIRS (2i, 2i+1).  The angles are formed in the kernel, in
+ * 64 bits, so that they lose nothing far into a context (|position * frequency| up to 2^31).
+ *
+ *   q, q_out         [B,T,Hq,d]  dtype   ([B,Hq,T,d] with SLA_FLAG_HEAD_MAJOR, rectangular batches only)
+ *   k, k_out         [B,T,Hk,d]  dtype   NULL with Hk == 0
+ *   frequencies      [rotary/2]  fp64    radians a token, one for each pair
+ *   positions        NULL: a sequence's tokens have positions 0, 1, ...;  else int32 [B]: the position of every sequence's first
+ *                    token;  with SLA_FLAG_TOKEN_POSITIONS int32 [B,T] (packed [T]): the position of every token
+ * q_out may be q and k_out k (the same address); nothing else may overlap.  sla_rotary_backward turns the cotangents of
+ * the outputs back (and scales them by m): dq_out, dk_out take the place of q, k and dq, dk that of q_out, k_out.
+ */
+#define SLA_FLAG_ADJACENT_PAIRS 2
+#define SLA_FLAG_TOKEN_POSITIONS 4
+typedef struct {
+    int32_t dtype;     /* sla_dtype of the tensors */
+    int32_t B, T;
+    int32_t Hq, Hk;    /* heads of q (1..1024) and of k (0..1024) */
+    int32_t d;         /* head width, a multiple of 8, 8..512 */
+    int32_t rotary;    /* elements that are turned, even, 2..d */
+    int32_t flags;     /* SLA_FLAG_HEAD_MAJOR, SLA_FLAG_ADJACENT_PAIRS, SLA_FLAG_TOKEN_POSITIONS */
+    float magnitude;   /* m; 1 for a plain turn */
+} sla_rotary_params;
+int sla_rotary(const sla_rotary_params* p, const void* q, const void* k, const double* frequencies,
+               const int32_t* positions, const int32_t* cu_seqlens, void* q_out, void* k_out, void* stream);
+int sla_rotary_backward(const sla_rotary_params* p, const void* dq_out, const void* dk_out, const double* frequencies,
+                        const int32_t* positions, const int32_t* cu_seqlens, void* dq, void* dk, void* stream);
+
+/*
+ * The read-out: every head's output of the mixer divided by its root mean square, weighted and gated,
+ *     n = x / sqrt(mean(x^2) + eps),   y = n w act(g)           act(g) = g sigmoid(g), sigmoid(g), or 1
+ * and its gradients from the same inputs and the cotangent dy of y (nothing is kept from the forward call):
+ *
+ *   x, dx    [B,T,H,dv]  dtype   with SLA_FLAG_HEAD_MAJOR [B,H,T,dv], as sla_forward leaves out there; rectangular batches only
+ *   g, dg    [B,T,H,dv]  dtype   NULL with SLA_GATE_NONE
+ *   y, dy    [B,T,H,dv]  dtype
+ *   w, dw    fp32: [dv], with SLA_FLAG_HEAD_WEIGHTS [H,dv]; both NULL: no weight.  dw is the sum over all tokens (and heads
+ *            that share it) in a fixed order; zeros for an empty batch
+ *   workspace  sla_norm_gate_backward_workspace_bytes(p, packed) bytes, 16-byte aligned, for dw (packed: with cu_seqlens);
+ *            contents undefined before and after, calls that share it must not overlap
+ * y may be g or, without SLA_FLAG_HEAD_MAJOR, x (the same address); nothing else may overlap.
+ */
+typedef enum { SLA_GATE_NONE = 0, SLA_GATE_SILU = 1, SLA_GATE_SIGMOID = 2 } sla_gate;
+#define SLA_FLAG_HEAD_WEIGHTS 2
+typedef struct {
+    int32_t dtype;   /* sla_dtype of the tensors */
+    int32_t B, T;
+    int32_t H;       /* heads, 1..1024 */
+    int32_t dv;      /* head width, a multiple of 8, 8..512 */
+    int32_t gate;    /* sla_gate */
+    int32_t flags;   /* SLA_FLAG_HEAD_MAJOR, SLA_FLAG_HEAD_WEIGHTS */
+    float eps;       /* >= 0 */
+} sla_norm_gate_params;
+int sla_norm_gate(const sla_norm_gate_params* p, const void* x, const void* g, const float* w, const int32_t* cu_seqlens,
+                  void* y, void* stream);
+int sla_norm_gate_backward(const sla_norm_gate_params* p, const void* x, const void* g, const float* w, const void* dy,
+                           const int32_t* cu_seqlens, void* dx, void* dg, float* dw, void* workspace,
+                           size_t workspace_bytes, void* stream);
+size_t sla_norm_gate_backward_workspace_bytes(const sla_norm_gate_params* p, int packed);
+
+/*
+ * The join of a block's output h with the residual stream x, and the norm in front of the next block:
+ *     u = h, or with w_after h / sqrt(mean(h^2) + eps) * w_after;   x' = x + scale * c * u;   y = x' / sqrt(mean(x'^2) + eps) * w_before
+ * (c = channel_scale, or 1; means over the width D; x' enters y before it is rounded to the stream's type).
+ *
+ *   x, x_out, dx, dx_out   [B,T,D]  x_dtype   the stream
+ *   h, y, dh, dy           [B,T,D]  dtype
+ *   w_after, channel_scale, w_before and their gradients  [D] fp32
+ * sla_join_norm: h NULL (then x_out, w_after, channel_scale too) only norms x; y NULL (then w_before too) only joins.
+ * x_out may be x, and y may be h (the same address); nothing else may overlap.
+ * sla_join_norm_backward works from x_out as the forward left it, and from h where w_after or channel_scale is given:
+ *   dy, w_before, dw_before, dx   all, or none where the forward had no y (the gradient of x is dx_out itself then)
+ *   dx_out     cotangent of x_out that later blocks send, or NULL (zero)
+ *   dh         written, or NULL where it is not wanted (required with w_after or channel_scale)
+ *   dw_after, dchannel_scale, dw_before   written, each where its weight is given: sums over all tokens in a fixed order; zeros for
+ *              an empty batch
+ *   workspace  sla_join_norm_backward_workspace_bytes(p, packed) bytes, as for sla_norm_gate_backward, for these sums
+ * dx may be dx_out, and dh may be dy or h (the same address); nothing else may overlap.
+ */
+typedef struct {
+    int32_t dtype;    /* sla_dtype of h, y and their gradients */
+    int32_t x_dtype;  /* sla_dtype of the stream and its gradients: dtype, or SLA_F32 */
+    int32_t B, T;
+    int32_t D;        /* width, a multiple of 8, 8..16384 */
+    float scale;
+    float eps;        /* >= 0 */
+} sla_join_norm_params;
+int sla_join_norm(const sla_join_norm_params* p, const void* x, const void* h, const float* w_after,
+                  const float* channel_scale, const float* w_before, const int32_t* cu_seqlens, void* x_out, void* y,
+                  void* stream);
+int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, const void* h, const float* w_after,
+                           const float* channel_scale, const float* w_before, const void* dy, const void* dx_out,
+                           const int32_t* cu_seqlens, void* dx, void* dh, float* dw_after, float* dchannel_scale,
+                           float* dw_before, void* workspace, size_t workspace_bytes, void* stream);
+size_t sla_join_norm_backward_workspace_bytes(const sla_join_norm_params* p, int packed);
+
 /* Bytes of workspace sla_forward_ws wants for *p on a device with that many compute units (0: none needed). */
 size_t sla_workspace_bytes(const sla_params* p, int compute_units);
 

@@ -12,6 +12,8 @@
                    against ``sla_backward``; fast enough for whole workloads.
 ``sla_prologue`` – gate projections, short convolution + SiLU (+ L2 normalisation) and their
                    backward, fp64 numpy; pinned by finite differences and library autograd.
+``sla_layer``    – rotary positions, the gated read-out norm, the residual join, and their gradients, fp64 numpy; pinned by
+                   finite differences.
 
 Nothing under the GPU package imports this package; only ``tests/``, the smoke
 check and the benchmark's cpu_baseline leg do.
@@ -25,7 +27,7 @@ from typing import Optional, Tuple
 
 import numpy as np
 
-from . import sla_backward, sla_numpy, sla_prologue  # noqa: F401
+from . import sla_backward, sla_layer, sla_numpy, sla_prologue  # noqa: F401
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _SRC = os.path.join(_HERE, "sla_oracle.c")

@@ -42,6 +42,25 @@ class SlaParams(ctypes.Structure):
     ]
 
 
+class SlaRotaryParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "B", "T", "Hq", "Hk", "d", "rotary", "flags")] + [
+        ("magnitude", ctypes.c_float)]
+
+
+class SlaNormGateParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "B", "T", "H", "dv", "gate", "flags")] + [("eps", ctypes.c_float)]
+
+
+class SlaJoinNormParams(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "x_dtype", "B", "T", "D")] + [
+        ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+FLAG_ADJACENT_PAIRS, FLAG_TOKEN_POSITIONS = 2, 4  # sla_rotary_params.flags
+FLAG_HEAD_WEIGHTS = 2  # sla_norm_gate_params.flags
+GATES = {"none": 0, "silu": 1, "sigmoid": 2}
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -111,6 +130,22 @@ def load_library():
     lib.sla_backward_chunks_workspace_bytes.argtypes = [pp, ctypes.c_int]
     lib.sla_backward_gdn_chunks_workspace_bytes.restype = ctypes.c_size_t
     lib.sla_backward_gdn_chunks_workspace_bytes.argtypes = [pp, ctypes.c_int]
+    rp, np_, jp = (ctypes.POINTER(t) for t in (SlaRotaryParams, SlaNormGateParams, SlaJoinNormParams))
+    for call in (lib.sla_rotary, lib.sla_rotary_backward):
+        call.restype = ctypes.c_int
+        call.argtypes = [rp] + [vp] * 8
+    lib.sla_norm_gate.restype = ctypes.c_int
+    lib.sla_norm_gate.argtypes = [np_] + [vp] * 6
+    lib.sla_norm_gate_backward.restype = ctypes.c_int
+    lib.sla_norm_gate_backward.argtypes = [np_] + [vp] * 9 + [ctypes.c_size_t, vp]
+    lib.sla_norm_gate_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.sla_norm_gate_backward_workspace_bytes.argtypes = [np_, ctypes.c_int]
+    lib.sla_join_norm.restype = ctypes.c_int
+    lib.sla_join_norm.argtypes = [jp] + [vp] * 9
+    lib.sla_join_norm_backward.restype = ctypes.c_int
+    lib.sla_join_norm_backward.argtypes = [jp] + [vp] * 14 + [ctypes.c_size_t, vp]
+    lib.sla_join_norm_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.sla_join_norm_backward_workspace_bytes.argtypes = [jp, ctypes.c_int]
     lib.sla_forward_workspace_bytes.restype = ctypes.c_size_t
     lib.sla_forward_workspace_bytes.argtypes = [pp, ctypes.c_int]
     lib.sla_workspace_bytes.restype = ctypes.c_size_t
@@ -823,3 +858,333 @@ def forward(
     if rc != 0:
         raise SlaError(rc, sla_status_string(rc))
     return out, final_state
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Around the mixer: rotary positions, the normalised and gated read-out, the join with the residual stream.
+
+def sla_rotary(params, q, k, frequencies, positions, cu_seqlens, q_out, k_out, stream) -> int:
+    """Raw call: integer device addresses (0/None = NULL) and a hipStream_t handle.  Returns the status code."""
+    pr = ctypes.byref(params) if params is not None else None
+    return int(load_library().sla_rotary(pr, _p(q), _p(k), _p(frequencies), _p(positions), _p(cu_seqlens), _p(q_out),
+                                         _p(k_out), _p(stream)))
+
+
+def sla_rotary_backward(params, dq_out, dk_out, frequencies, positions, cu_seqlens, dq, dk, stream) -> int:
+    """Raw call of the rotary gradient (same conventions as sla_rotary)."""
+    pr = ctypes.byref(params) if params is not None else None
+    return int(load_library().sla_rotary_backward(pr, _p(dq_out), _p(dk_out), _p(frequencies), _p(positions),
+                                                  _p(cu_seqlens), _p(dq), _p(dk), _p(stream)))
+
+
+def sla_norm_gate(params, x, g, w, cu_seqlens, y, stream) -> int:
+    """Raw call of the read-out norm (integer device addresses or None)."""
+    pr = ctypes.byref(params) if params is not None else None
+    return int(load_library().sla_norm_gate(pr, _p(x), _p(g), _p(w), _p(cu_seqlens), _p(y), _p(stream)))
+
+
+def sla_norm_gate_backward_workspace_bytes(params, packed: bool = False) -> int:
+    return int(load_library().sla_norm_gate_backward_workspace_bytes(ctypes.byref(params), int(bool(packed))))
+
+
+def sla_norm_gate_backward(params, x, g, w, dy, cu_seqlens, dx, dg, dw, workspace, workspace_bytes, stream) -> int:
+    """Raw call of the read-out norm's gradients (integer device addresses or None)."""
+    pr = ctypes.byref(params) if params is not None else None
+    return int(load_library().sla_norm_gate_backward(pr, _p(x), _p(g), _p(w), _p(dy), _p(cu_seqlens), _p(dx), _p(dg),
+                                                     _p(dw), _p(workspace), int(workspace_bytes), _p(stream)))
+
+
+def sla_join_norm(params, x, h, w_after, channel_scale, w_before, cu_seqlens, x_out, y, stream) -> int:
+    """Raw call of the residual join (integer device addresses or None)."""
+    pr = ctypes.byref(params) if params is not None else None
+    return int(load_library().sla_join_norm(pr, _p(x), _p(h), _p(w_after), _p(channel_scale), _p(w_before),
+                                            _p(cu_seqlens), _p(x_out), _p(y), _p(stream)))
+
+
+def sla_join_norm_backward_workspace_bytes(params, packed: bool = False) -> int:
+    return int(load_library().sla_join_norm_backward_workspace_bytes(ctypes.byref(params), int(bool(packed))))
+
+
+def sla_join_norm_backward(params, x_out, h, w_after, channel_scale, w_before, dy, dx_out, cu_seqlens, dx, dh, dw_after,
+                           dchannel_scale, dw_before, workspace, workspace_bytes, stream) -> int:
+    """Raw call of the residual join's gradients (integer device addresses or None)."""
+    pr = ctypes.byref(params) if params is not None else None
+    return int(load_library().sla_join_norm_backward(
+        pr, _p(x_out), _p(h), _p(w_after), _p(channel_scale), _p(w_before), _p(dy), _p(dx_out), _p(cu_seqlens), _p(dx),
+        _p(dh), _p(dw_after), _p(dchannel_scale), _p(dw_before), _p(workspace), int(workspace_bytes), _p(stream)))
+
+
+def _need(ok, text):
+    if not ok:
+        raise ValueError(text)
+
+
+def _tensor(name, t, like, shape, dtype):
+    """Refuses what the library could not check: a tensor of another device, type, shape or order."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}, but got "
+                         f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _run(call, t, *args):
+    """One call of the library on the current stream of t's device, with that device the current one; raises on a status."""
+    import torch
+
+    stream = _stream(t)
+    if torch._C._cuda_getDevice() == t.get_device():
+        rc = call(*args, stream)
+    else:
+        with torch.cuda.device(t.device):
+            rc = call(*args, stream)
+    if rc != 0:
+        raise SlaError(rc, sla_status_string(rc))
+
+
+def _element(name, t):
+    import torch
+
+    if t.dtype is torch.bfloat16:
+        return BF16
+    _need(t.dtype is torch.float32, f"{name}: expected bfloat16 or float32, but got {t.dtype}")
+    return F32
+
+
+def _batch(name, t, cu_seqlens, head_major=False):
+    """(B, T, H, width) of a tensor of head vectors: [B,T,H,d] ([B,H,T,d] head-major); [T,H,d] with cu_seqlens; [B,H,d]
+    without: one token of each of B sequences, as decode_step has them."""
+    import torch
+
+    _need(max(t.shape, default=0) < 1 << 31, f"{name}: {tuple(t.shape)} is out of range")
+    if cu_seqlens is not None:
+        _need(t.dim() == 3 and not head_major, f"{name}: a packed batch is [T,H,d]")
+        _need(cu_seqlens.dtype is torch.int32 and cu_seqlens.dim() == 1 and cu_seqlens.numel() >= 1
+              and cu_seqlens.is_contiguous() and cu_seqlens.get_device() == t.get_device(),
+              f"cu_seqlens: expected a contiguous int32 tensor [B+1] on {t.device}")
+        T, H, d = t.shape
+        return cu_seqlens.numel() - 1, T, H, d
+    if t.dim() == 3 and not head_major:
+        B, H, d = t.shape
+        return B, 1, H, d
+    _need(t.dim() == 4, f"{name}: expected [B,T,H,d], [T,H,d] with cu_seqlens or [B,H,d]")
+    B, T, H, d = t.shape
+    return (B, H, T, d) if head_major else (B, T, H, d)
+
+
+def rotary_frequencies(width: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
+                       original_length: int = 4096, fast: float = 32.0, slow: float = 1.0, device=None):
+    """(frequencies [width/2] float64 on ``device`` (default: the current GPU), magnitude) for ``rotary``: pair i turns by
+    base^(-2i/width) radians a token.  For contexts of ``factor`` times the trained ``original_length``: "linear" divides every
+    frequency by factor (position interpolation); "base" multiplies base by factor^(width/(width-2)), so that the slowest pair
+    is slowed by factor and the fastest not at all; "blend" slows the pairs that turn fewer than ``slow`` times in the trained
+    length, keeps those over ``fast`` times, goes from one to the other linearly in the turns, and scales what is turned by
+    0.1 ln(factor) + 1 (YaRN, arXiv 2309.00071)."""
+    import math
+
+    import torch
+
+    _need(width >= 2 and width % 2 == 0, f"width: expected an even number of elements, but got {width}")
+    _need(scaling in ("none", "linear", "base", "blend"), f"scaling: unknown {scaling!r}")
+    _need(factor > 0 and base > 0 and (scaling != "blend" or (factor >= 1 and 0 < slow < fast and original_length > 0)),
+          "factor, base, fast, slow or original_length out of range")
+    if scaling == "base" and width > 2:
+        base = base * factor ** (width / (width - 2))
+    f = torch.tensor([base ** (-2.0 * i / width) for i in range(width // 2)], dtype=torch.float64)
+    magnitude = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "blend":
+        turns = f * (original_length / (2.0 * math.pi))
+        keep = torch.clamp((turns - slow) / (fast - slow), 0.0, 1.0)
+        f = f * keep + f / factor * (1.0 - keep)
+        magnitude = 0.1 * math.log(factor) + 1.0
+    return f.to(device if device is not None else "cuda"), magnitude
+
+
+def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, magnitude, head_major, q_out, k_out):
+    import torch
+
+    B, T, Hq, d = _batch("q", q, cu_seqlens, head_major)
+    dtype, Hk = _element("q", q), 0
+    _tensor("q", q, q, q.shape, q.dtype)
+    if k is not None:
+        Bk, Tk, Hk, dk = _batch("k", k, cu_seqlens, head_major)
+        _need((Bk, Tk, dk) == (B, T, d), f"k: {tuple(k.shape)} does not go with q: {tuple(q.shape)}")
+        _tensor("k", k, q, k.shape, q.dtype)
+    _tensor("frequencies", frequencies, q, (frequencies.numel(),), torch.float64)
+    flags = (FLAG_HEAD_MAJOR if head_major else 0) | (FLAG_ADJACENT_PAIRS if adjacent else 0)
+    where = start
+    if start is not None:
+        _need(positions is None, "start and positions: give one of them")
+        _tensor("start", start, q, (B,), torch.int32)
+    elif positions is not None:
+        _tensor("positions", positions, q, (T,) if cu_seqlens is not None else (B, T) if q.dim() == 4 else (B,), torch.int32)
+        where, flags = positions, flags | FLAG_TOKEN_POSITIONS
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    else:
+        _tensor("q's output", q_out, q, q.shape, q.dtype)
+    if k is None:
+        _need(k_out is None, "an output for k, but no k")
+    elif k_out is None:
+        k_out = torch.empty_like(k)
+    else:
+        _tensor("k's output", k_out, q, k.shape, q.dtype)
+    params = SlaRotaryParams(dtype, B, T, Hq, Hk, d, 2 * frequencies.numel(), flags, magnitude)
+    _run(call, q, ctypes.byref(params), q.data_ptr(), _ptr(k), frequencies.data_ptr(), _ptr(where), _ptr(cu_seqlens),
+         q_out.data_ptr(), _ptr(k_out))
+    return q_out, k_out
+
+
+def rotary(q, k, frequencies, *, start=None, positions=None, cu_seqlens=None, adjacent: bool = False,
+           magnitude: float = 1.0, head_major: bool = False, q_out=None, k_out=None):
+    """Turns the first 2 * len(frequencies) elements of every head vector of q [B,T,Hq,d] and k [B,T,Hk,d] (or None) by
+    position * frequency (sla_rotary); returns (q_out, k_out).  Head vectors may also be [B,H,T,d] (head_major), [T,H,d] with
+    cu_seqlens int32 [B+1], or [B,H,d]: one token of each of B sequences.  Positions count from 0 in every sequence, or from
+    start int32 [B], or are positions int32 [B,T] ([T] packed, [B] for one token each).  frequencies float64, see
+    ``rotary_frequencies``.  q_out and k_out may be q and k."""
+    return _rotary(load_library().sla_rotary, q, k, frequencies, start, positions, cu_seqlens, adjacent, magnitude,
+                   head_major, q_out, k_out)
+
+
+def rotary_backward(dq_out, dk_out, frequencies, *, start=None, positions=None, cu_seqlens=None, adjacent: bool = False,
+                    magnitude: float = 1.0, head_major: bool = False, dq=None, dk=None):
+    """Gradients (dq, dk) of ``rotary`` from the cotangents of its outputs (arguments as there); dq may be dq_out."""
+    return _rotary(load_library().sla_rotary_backward, dq_out, dk_out, frequencies, start, positions, cu_seqlens, adjacent,
+                   magnitude, head_major, dq, dk)
+
+
+def _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major):
+    import torch
+
+    B, T, H, dv = _batch("x", x, cu_seqlens, head_major)
+    dtype = _element("x", x)
+    _tensor("x", x, x, x.shape, x.dtype)
+    shape = torch.Size((B, T, H, dv)) if head_major else x.shape  # of everything but x, dx
+    _need(gate in GATES, f"gate: unknown {gate!r}")
+    _need((g is not None) == (gate != "none"), f"gate {gate!r}: {'needs g' if g is None else 'takes no g'}")
+    if g is not None:
+        _tensor("g", g, x, shape, x.dtype)
+    flags = FLAG_HEAD_MAJOR if head_major else 0
+    if w is not None:
+        heads = w.dim() == 2
+        _tensor("w", w, x, (H, dv) if heads else (dv,), torch.float32)
+        flags |= FLAG_HEAD_WEIGHTS if heads else 0
+    return SlaNormGateParams(dtype, B, T, H, dv, GATES[gate], flags, eps), shape
+
+
+def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None, head_major: bool = False, out=None):
+    """The read-out behind the mixer: y = x / sqrt(mean(x^2) + eps) * w * act(g) over every head vector (sla_norm_gate).
+    x, g [B,T,H,dv] ([T,H,dv] with cu_seqlens, [B,H,dv] for one token each), w float32 [dv], [H,dv] or None; gate "silu",
+    "sigmoid" or "none" (then g is None).  head_major: x is [B,H,T,dv], g and y are [B,T,H,dv].  ``out`` may be g or, without
+    head_major, x."""
+    params, shape = _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major)
+    if out is None:
+        out = x.new_empty(shape)
+    else:
+        _tensor("out", out, x, shape, x.dtype)
+    _run(load_library().sla_norm_gate, x, ctypes.byref(params), x.data_ptr(), _ptr(g), _ptr(w), _ptr(cu_seqlens), out.data_ptr())
+    return out
+
+
+def norm_gate_backward(x, g, w, dy, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None, head_major: bool = False,
+                       workspace=None):
+    """Gradients of ``norm_gate`` for the cotangent dy of y, as a dict of new tensors: dx like x, dg like g (or None), dw like w
+    (or None).  ``workspace``: a tensor of sla_norm_gate_backward_workspace_bytes, else it is allocated here."""
+    import torch
+
+    params, shape = _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major)
+    _tensor("dy", dy, x, shape, x.dtype)
+    dx = torch.empty_like(x)
+    dg = None if g is None else torch.empty_like(g)
+    dw = None if w is None else torch.empty_like(w)
+    if workspace is None and dw is not None:
+        workspace = x.new_empty(max(sla_norm_gate_backward_workspace_bytes(params, cu_seqlens is not None), 16), dtype=torch.uint8)
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _run(load_library().sla_norm_gate_backward, x, ctypes.byref(params), x.data_ptr(), _ptr(g), _ptr(w), dy.data_ptr(),
+         _ptr(cu_seqlens), dx.data_ptr(), _ptr(dg), _ptr(dw), _ptr(workspace), size)
+    return {"dx": dx, "dg": dg, "dw": dw}
+
+
+def _join_args(x, of, w_after, channel_scale, w_before, scale, eps, cu_seqlens):
+    """Params for the stream x [..., D] and, where there are any, block tensors ``of`` {name: tensor}."""
+    import torch
+
+    _need(x.dim() >= 1, "x: expected [..., D]")
+    D = x.shape[-1]
+    x_dtype = dtype = _element("x", x)
+    _tensor("x", x, x, x.shape, x.dtype)
+    kind = None
+    for name, t in of.items():
+        if t is not None:
+            kind = kind or t.dtype
+            dtype = _element(name, t)
+            _tensor(name, t, x, x.shape, kind)
+    for name, t in (("w_after", w_after), ("channel_scale", channel_scale), ("w_before", w_before)):
+        if t is not None:
+            _tensor(name, t, x, (D,), torch.float32)
+    if cu_seqlens is not None:
+        _need(x.dim() == 2, "x: a packed batch is [T,D]")
+        _need(cu_seqlens.dtype is torch.int32 and cu_seqlens.dim() == 1 and cu_seqlens.numel() >= 1
+              and cu_seqlens.is_contiguous() and cu_seqlens.get_device() == x.get_device(),
+              f"cu_seqlens: expected a contiguous int32 tensor [B+1] on {x.device}")
+        return SlaJoinNormParams(dtype, x_dtype, cu_seqlens.numel() - 1, x.shape[0], D, scale, eps)
+    tokens = x.numel() // D if D else 0
+    _need(tokens < 1 << 31, f"x: {tuple(x.shape)} is out of range")
+    return SlaJoinNormParams(dtype, x_dtype, 1, tokens, D, scale, eps)
+
+
+def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float = 1.0, eps: float = 1e-5, cu_seqlens=None,
+              x_out=None, y=None, y_dtype=None):
+    """A block's output h joins the residual stream x, and the stream is normalised for the next block (sla_join_norm):
+    u = h, or h / rms(h) * w_after;  x_out = x + scale * channel_scale * u;  y = x_out / rms(x_out) * w_before.  x, h [..., D]
+    ([T,D] with cu_seqlens), x float32 or of h's type; weights float32 [D].  Returns (x_out, y).  h None: no join, x_out is x, and
+    y has y_dtype (default: x's type); w_before None: no norm, y is None.  ``x_out`` may be x and ``y`` may be h."""
+    import torch
+
+    _need(h is not None or (w_before is not None and w_after is None and channel_scale is None and x_out is None),
+          "h: needed, unless only the norm of x is asked for")
+    _need(w_before is not None or y is None, "an output y, but no w_before")
+    params = _join_args(x, {"h": h, "y": y}, w_after, channel_scale, w_before, scale, eps, cu_seqlens)
+    if h is not None:
+        if x_out is None:
+            x_out = torch.empty_like(x)
+        else:
+            _tensor("x_out", x_out, x, x.shape, x.dtype)
+    if w_before is not None and y is None:
+        y = torch.empty_like(x, dtype=h.dtype if h is not None else y_dtype or x.dtype)
+        params.dtype = _element("y", y)
+    _run(load_library().sla_join_norm, x, ctypes.byref(params), x.data_ptr(), _ptr(h), _ptr(w_after), _ptr(channel_scale),
+         _ptr(w_before), _ptr(cu_seqlens), _ptr(x_out), _ptr(y))
+    return (x if h is None else x_out), y
+
+
+def join_norm_backward(x_out, h, w_before, dy, dx_out=None, *, w_after=None, channel_scale=None, scale: float = 1.0,
+                       eps: float = 1e-5, cu_seqlens=None, workspace=None):
+    """Gradients of ``join_norm`` from its x_out, for the cotangents dy of y and dx_out of x_out (None: zero), as a dict:
+    dx, dh, dw_after, dchannel_scale, dw_before (None where the forward had no such input).  Without w_before (and dy) dx is
+    dx_out itself.  h is read only with w_after or channel_scale; None: the forward only normalised x.  ``workspace``: a tensor of
+    sla_join_norm_backward_workspace_bytes, else it is allocated here."""
+    import torch
+
+    _need((dy is None) == (w_before is None) and (dy is not None or dx_out is not None), "dy goes with w_before; without them dx_out")
+    _need(h is not None or (w_after is None and channel_scale is None), "h: needed with w_after or channel_scale")
+    params = _join_args(x_out, {"dy": dy, "h": h}, w_after, channel_scale, w_before, scale, eps, cu_seqlens)
+    if dx_out is not None:
+        _tensor("dx_out", dx_out, x_out, x_out.shape, x_out.dtype)
+    like = lambda t: None if t is None else torch.empty_like(t)
+    dx = dx_out if dy is None else torch.empty_like(x_out)
+    g = {"dx": dx, "dh": like(h), "dw_after": like(w_after), "dchannel_scale": like(channel_scale), "dw_before": like(w_before)}
+    if dy is None and h is None:
+        return g
+    sums = dy is not None or w_after is not None or channel_scale is not None
+    if workspace is None and sums:
+        workspace = x_out.new_empty(max(sla_join_norm_backward_workspace_bytes(params, cu_seqlens is not None), 16), dtype=torch.uint8)
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _run(load_library().sla_join_norm_backward, x_out, ctypes.byref(params), x_out.data_ptr(), _ptr(h), _ptr(w_after),
+         _ptr(channel_scale), _ptr(w_before), _ptr(dy), _ptr(dx_out), _ptr(cu_seqlens), None if dy is None else dx.data_ptr(),
+         _ptr(g["dh"]), _ptr(g["dw_after"]), _ptr(g["dchannel_scale"]), _ptr(g["dw_before"]), _ptr(workspace), size)
+    return g

@@ -1,0 +1,427 @@
+// The residual stream between two blocks of a layer stack for gfx950: a block's output h joins the stream x, behind a norm
+// of its own if it has one, and the next block's input is the stream's norm, in one pass,
+//     u = h  or  h / rms(h) * w_after,    x' = x + scale * c * u,    y = x' / rms(x') * w_before      rms(v) = sqrt(mean(v^2) + eps)
+// (c a scale per channel, or 1), and the gradients from x' for the cotangents dy of y and dx' of x',
+//     n = x' r,  dn = dy w_before,  dX = dx' + r (dn - n mean(dn n))           dx = dX,  dw_before = sum dy n
+//     m = h r_h, P = sum scale dX m,  dm = scale dX c w_after                  dw_after = c P,  dc = w_after P
+//     dh = r_h (dm - m mean(dm m))         or, without the norm behind the block, dh = scale dX c,  dc = sum scale dX h.
+//
+// Streaming passes over 4 (backward up to 6) tensors.  A row of the stream lies in the registers of one to sixteen waves, 8 V
+// elements a lane, from its first read to its last write, so nothing is read twice; a sum over it is a few lane exchanges
+// and, where waves share the row, one exchange through LDS.  x' goes into y before it is rounded to the stream's type.  The
+// backward's workgroups walk over rows with the sums for w_before and P in registers and leave one partial sum each; a
+// second kernel adds these in a fixed order: no atomics, so results do not change from run to run.
+#include "sla_row_ops.h"
+
+namespace sla {
+
+namespace {
+
+using namespace row_ops;
+
+constexpr int kMaxWidth = 16384;
+
+struct JoinArgs {
+    const void *x, *h, *dy, *dxo;
+    const float *w_after, *channel, *w_before;
+    void *xo, *y, *dx, *dh;
+    float* part;
+    const int32_t* cu;
+    int64_t tokens;
+    int B, D;
+    int row_waves;   // waves of a row
+    int rows;        // rows of a workgroup
+    float scale, eps, inv_d;
+};
+
+// Sums of N values over the lanes of a row, to all of them; every wave of the workgroup takes part the same number of times.
+// `flip` alternates between two halves of the exchange buffer, so that one barrier a sum is enough.
+template <int N>
+__device__ __forceinline__ void row_sums(float (&s)[N], int row_waves, float* red, int& flip) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = lanes_sum(s[i], 64);
+    if (row_waves == 1) return;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    float* r = red + flip * 16 * 4;
+    flip ^= 1;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r[wv * 4 + i] = s[i];
+    }
+    __syncthreads();
+    const int w0 = wv / row_waves * row_waves;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float t = 0.f;
+        for (int w = 0; w < row_waves; ++w) t += r[(w0 + w) * 4 + i];
+        s[i] = t;
+    }
+}
+
+template <bool XBF, bool HBF, int V>
+__global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
+    __shared__ float red[2 * 16 * 4];
+    int flip = 0;
+    const int wv = threadIdx.x >> 6, slot = wv / a.row_waves;
+    const int col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8;
+    int64_t first, end;
+    token_range(a.cu, a.B, a.tokens, first, end);
+    for (int64_t r0 = first + (int64_t)blockIdx.x * a.rows; r0 < end; r0 += (int64_t)gridDim.x * a.rows) {
+        const int64_t n = r0 + slot;
+        const size_t row = (size_t)n * a.D;
+        float x[V][8], h[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] = h[v][i] = 0.f;
+            const int j = col + v * next;
+            if (j < a.D && n < end) {
+                load8<XBF>(a.x, row + j, x[v]);
+                if (a.h) load8<HBF>(a.h, row + j, h[v]);
+            }
+        }
+        if (a.h) {
+            float rh = a.scale;
+            if (a.w_after) {
+                float s[1] = {0.f};
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[0] += h[v][i] * h[v][i];
+                row_sums(s, a.row_waves, red, flip);
+                rh *= inverse_root(s[0] * a.inv_d + a.eps);
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int j = col + v * next;
+                if (j >= a.D) continue;
+                float w[8], c[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = c[i] = 1.f;
+                if (a.w_after) load8<false>(a.w_after, j, w);
+                if (a.channel) load8<false>(a.channel, j, c);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[v][i] += h[v][i] * rh * w[i] * c[i];
+                if (n < end) store8<XBF>(a.xo, row + j, x[v]);
+            }
+        }
+        if (a.y) {
+            float s[1] = {0.f};
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[0] += x[v][i] * x[v][i];
+            row_sums(s, a.row_waves, red, flip);
+            const float r = inverse_root(s[0] * a.inv_d + a.eps);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int j = col + v * next;
+                if (j >= a.D || n >= end) continue;
+                float w[8];
+                load8<false>(a.w_before, j, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[v][i] *= r * w[i];
+                store8<HBF>(a.y, row + j, x[v]);
+            }
+        }
+    }
+}
+
+// SUMS: planes of partial sums, 1 for w_before alone, 2 with P.
+template <bool XBF, bool HBF, int V>
+__global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a) {
+    extern __shared__ float sums[];  // [rows - 1][2][64 * row_waves * V * 8], past the exchange buffer
+    float* red = sums;
+    int flip = 0;
+    const int wv = threadIdx.x >> 6, slot = wv / a.row_waves;
+    const int col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8;
+    const bool reads_h = a.w_after || a.channel;
+    float wb[V][8], pw[V][8], pp[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int j = col + v * next;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wb[v][i] = pw[v][i] = pp[v][i] = 0.f;
+        if (a.dy && j < a.D) load8<false>(a.w_before, j, wb[v]);
+    }
+    int64_t first, end;
+    token_range(a.cu, a.B, a.tokens, first, end);
+    for (int64_t r0 = first + (int64_t)blockIdx.x * a.rows; r0 < end; r0 += (int64_t)gridDim.x * a.rows) {
+        const int64_t n = r0 + slot;
+        const size_t row = (size_t)n * a.D;
+        const bool there = n < end;
+        float x[V][8], dy[V][8], dx[V][8], h[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[v][i] = dy[v][i] = dx[v][i] = h[v][i] = 0.f;
+            const int j = col + v * next;
+            if (j < a.D && there) {
+                if (a.dy) {
+                    load8<XBF>(a.x, row + j, x[v]);
+                    load8<HBF>(a.dy, row + j, dy[v]);
+                }
+                if (a.dxo) load8<XBF>(a.dxo, row + j, dx[v]);
+                if (reads_h) load8<HBF>(a.h, row + j, h[v]);
+            }
+        }
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[0] += x[v][i] * x[v][i];
+                s[1] += dy[v][i] * wb[v][i] * x[v][i];
+                s[2] += h[v][i] * h[v][i];
+            }
+        row_sums(s, a.row_waves, red, flip);
+        const float rh = a.w_after ? inverse_root(s[2] * a.inv_d + a.eps) : 1.f;
+        if (a.dy) {
+            const float r = inverse_root(s[0] * a.inv_d + a.eps), mean = s[1] * r * a.inv_d;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int j = col + v * next;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float n_ = x[v][i] * r;
+                    if (there) pw[v][i] += dy[v][i] * n_;  // a row that is not there has no finite n where eps is 0
+                    dx[v][i] += r * (dy[v][i] * wb[v][i] - n_ * mean);
+                }
+                if (j < a.D && there) store8<XBF>(a.dx, row + j, dx[v]);
+            }
+        }
+        if (!a.dh) continue;
+        float t[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = col + v * next;
+            float w[8], c[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = c[i] = 1.f;
+            if (j < a.D) {
+                if (a.w_after) load8<false>(a.w_after, j, w);
+                if (a.channel) load8<false>(a.channel, j, c);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float du = a.scale * dx[v][i];
+                h[v][i] *= rh;
+                if (there && reads_h) pp[v][i] += du * h[v][i];
+                dx[v][i] = du * c[i] * w[i];
+                t[0] += dx[v][i] * h[v][i];
+            }
+        }
+        if (a.w_after) row_sums(t, a.row_waves, red, flip);
+        const float mean = a.w_after ? t[0] * a.inv_d : 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = col + v * next;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dx[v][i] = rh * (dx[v][i] - h[v][i] * mean);
+            if (j < a.D && there) store8<HBF>(a.dh, row + j, dx[v]);
+        }
+    }
+    if (!a.part) return;
+    // one partial sum a workgroup: the rows beside the first leave theirs in LDS
+    float* lds = sums + 2 * 16 * 4;
+    const int planes = reads_h ? 2 : 1, width = next * V;
+    __syncthreads();
+    if (slot > 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                lds[(size_t)(slot - 1) * planes * width + col + v * next + i] = pw[v][i];
+                if (planes == 2) lds[(size_t)((slot - 1) * planes + 1) * width + col + v * next + i] = pp[v][i];
+            }
+    }
+    __syncthreads();
+    if (slot > 0) return;
+    float* out = a.part + (size_t)blockIdx.x * planes * a.D;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int j = col + v * next;
+        if (j >= a.D) continue;
+        for (int q = 0; q < a.rows - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                pw[v][i] += lds[(size_t)q * planes * width + j + i];
+                if (planes == 2) pp[v][i] += lds[(size_t)(q * planes + 1) * width + j + i];
+            }
+        store8<false>(out, j, pw[v]);
+        if (planes == 2) store8<false>(out, a.D + j, pp[v]);
+    }
+}
+
+// One workgroup: 16 adjacent columns of a plane; 64 threads a column group walk the parts.
+constexpr int kSumColumns = 16, kSumRows = 64;
+__global__ __launch_bounds__(kSumColumns * kSumRows) void sla_column_sums_kernel(const float* part, int nparts, int planes, int width,
+                                                                               float* out0, float* out1, const float* by1,
+                                                                               float* out2, const float* by2) {
+    __shared__ float red[kSumRows][kSumColumns + 1];
+    const int c = threadIdx.x % kSumColumns, rr = threadIdx.x / kSumColumns;
+    const int per_plane = (width + kSumColumns - 1) / kSumColumns;
+    const int plane = blockIdx.x / per_plane, j = (blockIdx.x - plane * per_plane) * kSumColumns + c;
+    float s = 0.f;
+    if (j < width) {
+#pragma unroll 4
+        for (int n = rr; n < nparts; n += kSumRows) s += part[((size_t)n * planes + plane) * width + j];
+    }
+    red[rr][c] = s;
+    __syncthreads();
+    for (int half = kSumRows / 2; half > 0; half /= 2) {
+        if (rr < half) red[rr][c] += red[rr + half][c];
+        __syncthreads();
+    }
+    if (rr == 0 && j < width) {
+        s = red[0][c];
+        if (plane == 0) {
+            if (out0) out0[j] = s;
+        } else {
+            if (out1) out1[j] = by1 ? s * by1[j] : s;
+            if (out2) out2[j] = by2 ? s * by2[j] : s;
+        }
+    }
+}
+
+int check_join(const sla_join_norm_params* p, const int32_t* cu) {
+    if (!p) return SLA_ERR_NULL;
+    if ((p->dtype != SLA_F32 && p->dtype != SLA_BF16) || (p->x_dtype != SLA_F32 && p->x_dtype != SLA_BF16)) return SLA_ERR_UNSUPPORTED;
+    if (p->dtype == SLA_F32 && p->x_dtype == SLA_BF16) return SLA_ERR_UNSUPPORTED;  // the stream is never narrower than the blocks
+    if (p->B < 0 || p->T < 0 || p->D < 8 || p->D > kMaxWidth || (p->D & 7) || !(p->eps >= 0.f)) return SLA_ERR_SHAPE;
+    if ((cu ? (int64_t)p->T : (int64_t)p->B * p->T) > (int64_t)1 << 30) return SLA_ERR_SHAPE;
+    if (!aligned(cu, 4)) return SLA_ERR_ALIGN;
+    return SLA_OK;
+}
+
+int64_t tokens_of(const sla_join_norm_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
+
+// How a row lies over lanes: v pieces of eight a lane.  Four rows of a wave each as long as that takes at most `most` pieces,
+// else more waves a row.
+struct Split {
+    int v, row_waves, rows, threads;
+};
+Split split(int D, int most) {
+    Split s{1, 1, 1, 256};
+    while (s.row_waves < 16 && s.row_waves * 64 * 8 * most < D) s.row_waves *= 2;
+    while (s.row_waves * 64 * 8 * s.v < D) s.v *= 2;
+    s.rows = s.row_waves < 4 ? 4 / s.row_waves : 1;
+    s.threads = s.row_waves < 4 ? 256 : s.row_waves * 64;
+    return s;
+}
+
+Split forward_split(int D, int64_t tokens) {
+    Split s = split(D, 4);
+    if (tokens * s.row_waves < (int64_t)kComputeUnits * 8) s = split(D, 1);  // few rows: as many lanes on each as there are pieces
+    return s;
+}
+
+constexpr int kBackwardMost = 2;
+constexpr int64_t kBackwardGroups = kComputeUnits * 4;
+unsigned backward_workgroups(const Split& s, int64_t tokens) {
+    const int64_t n = (tokens + s.rows - 1) / s.rows;
+    return (unsigned)(n < kBackwardGroups ? n : kBackwardGroups);
+}
+
+}  // namespace
+
+int launch_column_sums(const float* part, int nparts, int planes, int width, float* out0, float* out1, const float* by1,
+                       float* out2, const float* by2, hipStream_t stream) {
+    const unsigned per_plane = (unsigned)((width + kSumColumns - 1) / kSumColumns);
+    hipLaunchKernelGGL(sla_column_sums_kernel, dim3(per_plane * planes), dim3(kSumColumns * kSumRows), 0, stream, part,
+                       nparts, planes, width, out0, out1, by1, out2, by2);
+    return hipGetLastError() == hipSuccess ? SLA_OK : SLA_ERR_HIP;
+}
+
+}  // namespace sla
+
+extern "C" {
+
+int sla_join_norm(const sla_join_norm_params* p, const void* x, const void* h, const float* w_after, const float* channel_scale,
+                  const float* w_before, const int32_t* cu_seqlens, void* x_out, void* y, void* stream) {
+    using namespace sla;
+    const int rc = check_join(p, cu_seqlens);
+    if (rc != SLA_OK) return rc;
+    const bool work = p->B > 0 && p->T > 0;
+    if (work && (!x || (!h && !y))) return SLA_ERR_NULL;
+    if (work && ((h != nullptr) != (x_out != nullptr) || (y != nullptr) != (w_before != nullptr))) return SLA_ERR_NULL;
+    if (work && !h && (w_after || channel_scale)) return SLA_ERR_NULL;
+    const void* ptrs[] = {x, h, w_after, channel_scale, w_before, x_out, y};
+    for (const void* q : ptrs)
+        if (!aligned(q, 16)) return SLA_ERR_ALIGN;
+    if (!work) return SLA_OK;
+    JoinArgs a{};
+    a.x = x; a.h = h; a.w_after = w_after; a.channel = channel_scale; a.w_before = w_before; a.xo = x_out; a.y = y;
+    a.cu = cu_seqlens; a.tokens = tokens_of(*p, cu_seqlens); a.B = p->B; a.D = p->D;
+    a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.f / p->D;
+    const Split s = forward_split(p->D, a.tokens);
+    a.row_waves = s.row_waves; a.rows = s.rows;
+    const int64_t blocks = (a.tokens + s.rows - 1) / s.rows;
+    const dim3 grid((unsigned)(blocks < kComputeUnits * 64 ? blocks : kComputeUnits * 64));
+#define SLA_JN(X, Y, V) hipLaunchKernelGGL((sla_join_norm_kernel<X, Y, V>), grid, dim3(s.threads), 0, (hipStream_t)stream, a)
+#define SLA_JN_V(X, Y) \
+    if (s.v == 1) SLA_JN(X, Y, 1); else if (s.v == 2) SLA_JN(X, Y, 2); else SLA_JN(X, Y, 4)
+    if (p->dtype == SLA_F32) { SLA_JN_V(false, false); }
+    else if (p->x_dtype == SLA_F32) { SLA_JN_V(false, true); }
+    else { SLA_JN_V(true, true); }
+#undef SLA_JN_V
+#undef SLA_JN
+    return hipGetLastError() == hipSuccess ? SLA_OK : SLA_ERR_HIP;
+}
+
+size_t sla_join_norm_backward_workspace_bytes(const sla_join_norm_params* p, int packed) {
+    using namespace sla;
+    if (check_join(p, nullptr) != SLA_OK || p->B == 0 || p->T == 0) return 0;
+    return (size_t)backward_workgroups(split(p->D, kBackwardMost), tokens_of(*p, packed)) * 2 * p->D * sizeof(float);
+}
+
+int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, const void* h, const float* w_after,
+                           const float* channel_scale, const float* w_before, const void* dy, const void* dx_out,
+                           const int32_t* cu_seqlens, void* dx, void* dh, float* dw_after, float* dchannel_scale,
+                           float* dw_before, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace sla;
+    const int rc = check_join(p, cu_seqlens);
+    if (rc != SLA_OK) return rc;
+    const bool work = p->B > 0 && p->T > 0, reads_h = w_after || channel_scale;
+    // dy with the norm's weight and everything that flows from it; without it dx would be dx_out itself
+    if ((dy != nullptr) != (w_before != nullptr) || (w_before != nullptr) != (dw_before != nullptr)) {
+        if (work || (w_before != nullptr) != (dw_before != nullptr)) return SLA_ERR_NULL;
+    }
+    if ((w_after != nullptr) != (dw_after != nullptr) || (channel_scale != nullptr) != (dchannel_scale != nullptr)) return SLA_ERR_NULL;
+    if (work && ((dy != nullptr) != (dx != nullptr) || (dy && !x_out) || (!dy && !dx_out))) return SLA_ERR_NULL;
+    if (work && ((reads_h && (!h || !dh)) || (!dx && !dh))) return SLA_ERR_NULL;
+    const void* ptrs[] = {x_out, h, w_after, channel_scale, w_before, dy, dx_out, dx, dh, dw_after, dchannel_scale, dw_before, workspace};
+    for (const void* q : ptrs)
+        if (!aligned(q, 16)) return SLA_ERR_ALIGN;
+    const bool sums = dw_before || dw_after || dchannel_scale;
+    const int planes = reads_h ? 2 : 1;
+    if (!work)
+        return sums ? launch_column_sums(nullptr, 0, planes, p->D, dw_before, dw_after, nullptr, dchannel_scale, nullptr, (hipStream_t)stream)
+                    : SLA_OK;
+    if (sums && (!workspace || workspace_bytes < sla_join_norm_backward_workspace_bytes(p, cu_seqlens != nullptr)))
+        return SLA_ERR_WORKSPACE;
+    JoinArgs a{};
+    a.x = x_out; a.h = h; a.w_after = w_after; a.channel = channel_scale; a.w_before = w_before; a.dy = dy; a.dxo = dx_out;
+    a.dx = dx; a.dh = dh; a.part = sums ? (float*)workspace : nullptr;
+    a.cu = cu_seqlens; a.tokens = tokens_of(*p, cu_seqlens); a.B = p->B; a.D = p->D;
+    a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.f / p->D;
+    const Split s = split(p->D, kBackwardMost);
+    a.row_waves = s.row_waves; a.rows = s.rows;
+    const unsigned blocks = backward_workgroups(s, a.tokens);
+    const size_t lds = (2 * 16 * 4 + (size_t)(s.rows - 1) * planes * s.row_waves * 64 * 8 * s.v) * sizeof(float);
+#define SLA_JN(X, Y, V) \
+    hipLaunchKernelGGL((sla_join_norm_backward_kernel<X, Y, V>), dim3(blocks), dim3(s.threads), lds, (hipStream_t)stream, a)
+#define SLA_JN_V(X, Y) \
+    if (s.v == 1) SLA_JN(X, Y, 1); else SLA_JN(X, Y, 2)
+    if (p->dtype == SLA_F32) { SLA_JN_V(false, false); }
+    else if (p->x_dtype == SLA_F32) { SLA_JN_V(false, true); }
+    else { SLA_JN_V(true, true); }
+#undef SLA_JN_V
+#undef SLA_JN
+    if (hipGetLastError() != hipSuccess) return SLA_ERR_HIP;
+    if (!sums) return SLA_OK;
+    return launch_column_sums((const float*)workspace, (int)blocks, planes, p->D, dw_before, dw_after, channel_scale, dchannel_scale,
+                              w_after, (hipStream_t)stream);
+}
+
+}  // extern "C"
