@@ -127,44 +127,80 @@ __global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
     }
 }
 
-// SUMS: planes of partial sums, 1 for w_before alone, 2 with P.
+// With V == 1 the vectors of weights stay in registers and the next row's loads are under way while a row is worked on; with more
+// (rows over 4096, up to 1024 threads) there are no registers for either.
 template <bool XBF, bool HBF, int V>
-__global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a) {
-    extern __shared__ float sums[];  // [rows - 1][2][64 * row_waves * V * 8], past the exchange buffer
-    float* red = sums;
+__global__ __launch_bounds__(V == 1 ? 512 : 1024) void sla_join_norm_backward_kernel(JoinArgs a) {
+    extern __shared__ float red[];  // the exchange buffer; after it [rows - 1][planes][row_waves * 64 * 8 * V] sums
     int flip = 0;
     const int wv = threadIdx.x >> 6, slot = wv / a.row_waves;
     const int col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8;
     const bool reads_h = a.w_after || a.channel;
-    float wb[V][8], pw[V][8], pp[V][8];
+    Raw8<XBF> x_[V], dxo_[V];
+    Raw8<HBF> dy_[V], h_[V];
+    float wb[V][8], cw[V][8], pw[V][8], pp[V][8];
+    // w_before (0 without dy) and scale * channel * w_after at column j; past the row's end nothing is read
+    auto weights = [&](int v, int j) {
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            wb[v][i] = 0.f;
+            cw[v][i] = a.scale;
+        }
+        if (j >= a.D) return;
+        if (a.dy) load8<false>(a.w_before, j, wb[v]);
+        if (a.w_after) {
+            load8<false>(a.w_after, j, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) cw[v][i] *= w[i];
+        }
+        if (a.channel) {
+            load8<false>(a.channel, j, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) cw[v][i] *= w[i];
+        }
+    };
+    auto fetch = [&](int64_t n) {
+        const size_t row = (size_t)n * a.D;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = col + v * next;
+            if (j >= a.D) continue;
+            if (a.dy) {
+                fetch8(a.x, row + j, x_[v]);
+                fetch8(a.dy, row + j, dy_[v]);
+            }
+            if (a.dxo) fetch8(a.dxo, row + j, dxo_[v]);
+            if (reads_h) fetch8(a.h, row + j, h_[v]);
+        }
+    };
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int j = col + v * next;
+        x_[v] = {}; dxo_[v] = {}; dy_[v] = {}; h_[v] = {};  // what is never fetched counts as zero
 #pragma unroll
-        for (int i = 0; i < 8; ++i) wb[v][i] = pw[v][i] = pp[v][i] = 0.f;
-        if (a.dy && j < a.D) load8<false>(a.w_before, j, wb[v]);
+        for (int i = 0; i < 8; ++i) pw[v][i] = pp[v][i] = 0.f;
+        if (V == 1) weights(v, col + v * next);
     }
     int64_t first, end;
     token_range(a.cu, a.B, a.tokens, first, end);
-    for (int64_t r0 = first + (int64_t)blockIdx.x * a.rows; r0 < end; r0 += (int64_t)gridDim.x * a.rows) {
+    const int64_t step = (int64_t)gridDim.x * a.rows;
+    int64_t r0 = first + (int64_t)blockIdx.x * a.rows;
+    if (V == 1 && r0 + slot < end) fetch(r0 + slot);
+    for (; r0 < end; r0 += step) {
         const int64_t n = r0 + slot;
         const size_t row = (size_t)n * a.D;
-        const bool there = n < end;
+        const bool there = n < end;  // where not, the lanes hold some other row: nothing of it is stored or summed
+        if (V > 1 && there) fetch(n);
         float x[V][8], dy[V][8], dx[V][8], h[V][8];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[v][i] = dy[v][i] = dx[v][i] = h[v][i] = 0.f;
-            const int j = col + v * next;
-            if (j < a.D && there) {
-                if (a.dy) {
-                    load8<XBF>(a.x, row + j, x[v]);
-                    load8<HBF>(a.dy, row + j, dy[v]);
-                }
-                if (a.dxo) load8<XBF>(a.dxo, row + j, dx[v]);
-                if (reads_h) load8<HBF>(a.h, row + j, h[v]);
-            }
+            if (V > 1) weights(v, col + v * next);
+            unpack8(x_[v], x[v]);
+            unpack8(dy_[v], dy[v]);
+            unpack8(dxo_[v], dx[v]);
+            unpack8(h_[v], h[v]);
         }
+        if (V == 1 && n + step < end) fetch(n + step);
         float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -184,7 +220,7 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float n_ = x[v][i] * r;
-                    if (there) pw[v][i] += dy[v][i] * n_;  // a row that is not there has no finite n where eps is 0
+                    if (there) pw[v][i] += dy[v][i] * n_;
                     dx[v][i] += r * (dy[v][i] * wb[v][i] - n_ * mean);
                 }
                 if (j < a.D && there) store8<XBF>(a.dx, row + j, dx[v]);
@@ -194,20 +230,11 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
         float t[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int j = col + v * next;
-            float w[8], c[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = c[i] = 1.f;
-            if (j < a.D) {
-                if (a.w_after) load8<false>(a.w_after, j, w);
-                if (a.channel) load8<false>(a.channel, j, c);
-            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float du = a.scale * dx[v][i];
                 h[v][i] *= rh;
-                if (there && reads_h) pp[v][i] += du * h[v][i];
-                dx[v][i] = du * c[i] * w[i];
+                if (there) pp[v][i] += dx[v][i] * h[v][i];
+                dx[v][i] *= cw[v][i];
                 t[0] += dx[v][i] * h[v][i];
             }
         }
@@ -223,17 +250,14 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
     }
     if (!a.part) return;
     // one partial sum a workgroup: the rows beside the first leave theirs in LDS
-    float* lds = sums + 2 * 16 * 4;
+    float* lds = red + 2 * 16 * 4;
     const int planes = reads_h ? 2 : 1, width = next * V;
-    __syncthreads();
     if (slot > 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                lds[(size_t)(slot - 1) * planes * width + col + v * next + i] = pw[v][i];
-                if (planes == 2) lds[(size_t)((slot - 1) * planes + 1) * width + col + v * next + i] = pp[v][i];
-            }
+        for (int v = 0; v < V; ++v) {
+            store8<false>(lds, (size_t)(slot - 1) * planes * width + col + v * next, pw[v]);
+            if (planes == 2) store8<false>(lds, (size_t)((slot - 1) * planes + 1) * width + col + v * next, pp[v]);
+        }
     }
     __syncthreads();
     if (slot > 0) return;
@@ -242,45 +266,50 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
     for (int v = 0; v < V; ++v) {
         const int j = col + v * next;
         if (j >= a.D) continue;
-        for (int q = 0; q < a.rows - 1; ++q)
+        for (int q = 0; q < a.rows - 1; ++q) {
+            float u[8];
+            load8<false>(lds, (size_t)q * planes * width + j, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                pw[v][i] += lds[(size_t)q * planes * width + j + i];
-                if (planes == 2) pp[v][i] += lds[(size_t)(q * planes + 1) * width + j + i];
+            for (int i = 0; i < 8; ++i) pw[v][i] += u[i];
+            if (planes == 2) {
+                load8<false>(lds, (size_t)(q * planes + 1) * width + j, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) pp[v][i] += u[i];
             }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pp[v][i] *= a.scale;
         store8<false>(out, j, pw[v]);
         if (planes == 2) store8<false>(out, a.D + j, pp[v]);
     }
 }
 
-// One workgroup: 16 adjacent columns of a plane; 64 threads a column group walk the parts.
+// A workgroup sums 16 adjacent columns of a plane: 64 threads a column, four of them in a wave.
 constexpr int kSumColumns = 16, kSumRows = 64;
 __global__ __launch_bounds__(kSumColumns * kSumRows) void sla_column_sums_kernel(const float* part, int nparts, int planes, int width,
                                                                                float* out0, float* out1, const float* by1,
                                                                                float* out2, const float* by2) {
-    __shared__ float red[kSumRows][kSumColumns + 1];
-    const int c = threadIdx.x % kSumColumns, rr = threadIdx.x / kSumColumns;
+    __shared__ float red[kSumRows / 4][kSumColumns];
+    const int c = threadIdx.x % kSumColumns, rr = threadIdx.x / kSumColumns, wv = threadIdx.x >> 6;
     const int per_plane = (width + kSumColumns - 1) / kSumColumns;
     const int plane = blockIdx.x / per_plane, j = (blockIdx.x - plane * per_plane) * kSumColumns + c;
     float s = 0.f;
     if (j < width) {
-#pragma unroll 4
+#pragma unroll 8
         for (int n = rr; n < nparts; n += kSumRows) s += part[((size_t)n * planes + plane) * width + j];
     }
-    red[rr][c] = s;
+    s = lane_ops::all_groups(s);
+    if (threadIdx.x % 64 < kSumColumns) red[wv][c] = s;
     __syncthreads();
-    for (int half = kSumRows / 2; half > 0; half /= 2) {
-        if (rr < half) red[rr][c] += red[rr + half][c];
-        __syncthreads();
-    }
-    if (rr == 0 && j < width) {
-        s = red[0][c];
-        if (plane == 0) {
-            if (out0) out0[j] = s;
-        } else {
-            if (out1) out1[j] = by1 ? s * by1[j] : s;
-            if (out2) out2[j] = by2 ? s * by2[j] : s;
-        }
+    if (rr > 0 || j >= width) return;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < kSumRows / 4; ++w) s += red[w][c];
+    if (plane == 0) {
+        if (out0) out0[j] = s;
+    } else {
+        if (out1) out1[j] = by1 ? s * by1[j] : s;
+        if (out2) out2[j] = by2 ? s * by2[j] : s;
     }
 }
 
@@ -316,8 +345,20 @@ Split forward_split(int D, int64_t tokens) {
     return s;
 }
 
-constexpr int kBackwardMost = 2;
-constexpr int64_t kBackwardGroups = kComputeUnits * 4;
+// The backward's: one piece a lane up to 4096 columns, and eight waves a workgroup (sixteen where a row takes them).
+Split backward_split(int D) {
+    Split s{1, 1, 1, 512};
+    while (s.row_waves < 8 && s.row_waves * 64 * 8 < D) s.row_waves *= 2;
+    if (s.row_waves * 64 * 8 < D) {
+        s.v = 2;
+        if (s.row_waves * 64 * 8 * 2 < D) s.row_waves = 16;
+    }
+    s.rows = s.row_waves < 8 ? 8 / s.row_waves : 1;
+    if (s.row_waves == 16) s.threads = 1024;
+    return s;
+}
+
+constexpr int64_t kBackwardGroups = kComputeUnits * 2;  // workgroups, and with them partial sums
 unsigned backward_workgroups(const Split& s, int64_t tokens) {
     const int64_t n = (tokens + s.rows - 1) / s.rows;
     return (unsigned)(n < kBackwardGroups ? n : kBackwardGroups);
@@ -372,7 +413,7 @@ int sla_join_norm(const sla_join_norm_params* p, const void* x, const void* h, c
 size_t sla_join_norm_backward_workspace_bytes(const sla_join_norm_params* p, int packed) {
     using namespace sla;
     if (check_join(p, nullptr) != SLA_OK || p->B == 0 || p->T == 0) return 0;
-    return (size_t)backward_workgroups(split(p->D, kBackwardMost), tokens_of(*p, packed)) * 2 * p->D * sizeof(float);
+    return (size_t)backward_workgroups(backward_split(p->D), tokens_of(*p, packed)) * 2 * p->D * sizeof(float);
 }
 
 int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, const void* h, const float* w_after,
@@ -405,7 +446,7 @@ int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, con
     a.dx = dx; a.dh = dh; a.part = sums ? (float*)workspace : nullptr;
     a.cu = cu_seqlens; a.tokens = tokens_of(*p, cu_seqlens); a.B = p->B; a.D = p->D;
     a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.f / p->D;
-    const Split s = split(p->D, kBackwardMost);
+    const Split s = backward_split(p->D);
     a.row_waves = s.row_waves; a.rows = s.rows;
     const unsigned blocks = backward_workgroups(s, a.tokens);
     const size_t lds = (2 * 16 * 4 + (size_t)(s.rows - 1) * planes * s.row_waves * 64 * 8 * s.v) * sizeof(float);

@@ -16,23 +16,42 @@ using lane_ops::u4;
 // The chip the library is built for; sizes of grids and workspaces must not depend on the current device.
 constexpr int kComputeUnits = 256;
 
+// Eight elements as they lie in memory, for loads that are waited for later.
+template <bool BF16>
+struct Raw8;
+template <>
+struct Raw8<true> {
+    u4 v;
+};
+template <>
+struct Raw8<false> {
+    f4 a, b;
+};
+__device__ __forceinline__ void fetch8(const void* x, size_t off, Raw8<true>& r) { r.v = *(const u4*)((const uint16_t*)x + off); }
+__device__ __forceinline__ void fetch8(const void* x, size_t off, Raw8<false>& r) {
+    r.a = *(const f4*)((const float*)x + off);
+    r.b = *(const f4*)((const float*)x + off + 4);
+}
+__device__ __forceinline__ void unpack8(const Raw8<true>& r, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = lane_ops::bf_lo(r.v[i]);
+        f[2 * i + 1] = lane_ops::bf_hi(r.v[i]);
+    }
+}
+__device__ __forceinline__ void unpack8(const Raw8<false>& r, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = r.a[i];
+        f[4 + i] = r.b[i];
+    }
+}
+
 template <bool BF16>
 __device__ __forceinline__ void load8(const void* x, size_t off, float (&f)[8]) {
-    if constexpr (BF16) {
-        const u4 v = *(const u4*)((const uint16_t*)x + off);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = lane_ops::bf_lo(v[i]);
-            f[2 * i + 1] = lane_ops::bf_hi(v[i]);
-        }
-    } else {
-        const f4 a = *(const f4*)((const float*)x + off), b = *(const f4*)((const float*)x + off + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[i] = a[i];
-            f[4 + i] = b[i];
-        }
-    }
+    Raw8<BF16> r;
+    fetch8(x, off, r);
+    unpack8(r, f);
 }
 
 template <bool BF16>
