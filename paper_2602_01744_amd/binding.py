@@ -8,6 +8,7 @@ passes ``data_ptr()``s and the current stream to ``sla_forward``.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import sys
 from typing import Optional, Tuple
@@ -919,10 +920,10 @@ def _need(ok, text):
         raise ValueError(text)
 
 
-def _tensor(name, t, like, shape, dtype):
+def _tensor(name, t, device, shape, dtype):
     """Refuses what the library could not check: a tensor of another device, type, shape or order."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != like.get_device():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {like.device}, but got "
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {device}, but got "
                          f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
@@ -930,11 +931,22 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# Parameter blocks by value: a token's host time is part of every step, and building one costs a microsecond.
+@functools.lru_cache(maxsize=1024)
+def _params(kind, *fields):
+    return ctypes.byref(kind(*fields))
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace_size(kind, *fields, packed):
+    query = sla_norm_gate_backward_workspace_bytes if kind is SlaNormGateParams else sla_join_norm_backward_workspace_bytes
+    return max(query(kind(*fields), packed), 16)
+
+
 def _run(call, t, *args):
     """One call of the library on the current stream of t's device, with that device the current one; raises on a status."""
-    import torch
-
     stream = _stream(t)
+    torch = sys.modules["torch"]
     if torch._C._cuda_getDevice() == t.get_device():
         rc = call(*args, stream)
     else:
@@ -944,34 +956,36 @@ def _run(call, t, *args):
         raise SlaError(rc, sla_status_string(rc))
 
 
-def _element(name, t):
-    import torch
-
-    if t.dtype is torch.bfloat16:
+def _element(name, dtype):
+    torch = sys.modules["torch"]
+    if dtype is torch.bfloat16:
         return BF16
-    _need(t.dtype is torch.float32, f"{name}: expected bfloat16 or float32, but got {t.dtype}")
+    if dtype is not torch.float32:
+        raise ValueError(f"{name}: expected bfloat16 or float32, but got {dtype}")
     return F32
 
 
-def _batch(name, t, cu_seqlens, head_major=False):
+def _sequences(name, cu_seqlens, device):
+    """The number of sequences that cu_seqlens bounds."""
+    _need(cu_seqlens.dim() == 1 and cu_seqlens.numel() >= 1, f"{name}: cu_seqlens is [B+1]")
+    _tensor("cu_seqlens", cu_seqlens, device, cu_seqlens.shape, sys.modules["torch"].int32)
+    return cu_seqlens.numel() - 1
+
+
+def _batch(name, t, cu_seqlens, head_major):
     """(B, T, H, width) of a tensor of head vectors: [B,T,H,d] ([B,H,T,d] head-major); [T,H,d] with cu_seqlens; [B,H,d]
     without: one token of each of B sequences, as decode_step has them."""
-    import torch
-
-    _need(max(t.shape, default=0) < 1 << 31, f"{name}: {tuple(t.shape)} is out of range")
+    shape = t.shape
     if cu_seqlens is not None:
-        _need(t.dim() == 3 and not head_major, f"{name}: a packed batch is [T,H,d]")
-        _need(cu_seqlens.dtype is torch.int32 and cu_seqlens.dim() == 1 and cu_seqlens.numel() >= 1
-              and cu_seqlens.is_contiguous() and cu_seqlens.get_device() == t.get_device(),
-              f"cu_seqlens: expected a contiguous int32 tensor [B+1] on {t.device}")
-        T, H, d = t.shape
-        return cu_seqlens.numel() - 1, T, H, d
-    if t.dim() == 3 and not head_major:
-        B, H, d = t.shape
-        return B, 1, H, d
-    _need(t.dim() == 4, f"{name}: expected [B,T,H,d], [T,H,d] with cu_seqlens or [B,H,d]")
-    B, T, H, d = t.shape
-    return (B, H, T, d) if head_major else (B, T, H, d)
+        _need(len(shape) == 3 and not head_major, f"{name}: a packed batch is [T,H,d]")
+        sizes = (_sequences(name, cu_seqlens, t.get_device()), *shape)
+    elif len(shape) == 4:
+        sizes = (shape[0], shape[2], shape[1], shape[3]) if head_major else tuple(shape)
+    else:
+        _need(len(shape) == 3 and not head_major, f"{name}: expected [B,T,H,d], [T,H,d] with cu_seqlens or [B,H,d]")
+        sizes = (shape[0], 1, shape[1], shape[2])
+    _need(max(sizes) < 1 << 31, f"{name}: {tuple(shape)} is out of range")
+    return sizes
 
 
 def rotary_frequencies(width: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
@@ -1005,37 +1019,36 @@ def rotary_frequencies(width: int, base: float = 10000.0, *, scaling: str = "non
 
 
 def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, magnitude, head_major, q_out, k_out):
-    import torch
-
+    torch = sys.modules["torch"]
+    device, el, Hk = q.get_device(), q.dtype, 0
     B, T, Hq, d = _batch("q", q, cu_seqlens, head_major)
-    dtype, Hk = _element("q", q), 0
-    _tensor("q", q, q, q.shape, q.dtype)
+    _tensor("q", q, device, q.shape, el)
     if k is not None:
-        Bk, Tk, Hk, dk = _batch("k", k, cu_seqlens, head_major)
-        _need((Bk, Tk, dk) == (B, T, d), f"k: {tuple(k.shape)} does not go with q: {tuple(q.shape)}")
-        _tensor("k", k, q, k.shape, q.dtype)
-    _tensor("frequencies", frequencies, q, (frequencies.numel(),), torch.float64)
+        Bk, Tk, Hk, dk = _batch("k", k, cu_seqlens, head_major) if k.shape != q.shape else (B, T, Hq, d)
+        _need(Bk == B and Tk == T and dk == d, f"k: {tuple(k.shape)} does not go with q: {tuple(q.shape)}")
+        _tensor("k", k, device, k.shape, el)
+    pairs = frequencies.numel()
+    _tensor("frequencies", frequencies, device, (pairs,), torch.float64)
     flags = (FLAG_HEAD_MAJOR if head_major else 0) | (FLAG_ADJACENT_PAIRS if adjacent else 0)
     where = start
     if start is not None:
         _need(positions is None, "start and positions: give one of them")
-        _tensor("start", start, q, (B,), torch.int32)
+        _tensor("start", start, device, (B,), torch.int32)
     elif positions is not None:
-        _tensor("positions", positions, q, (T,) if cu_seqlens is not None else (B, T) if q.dim() == 4 else (B,), torch.int32)
+        _tensor("positions", positions, device, (T,) if cu_seqlens is not None else (B, T) if q.dim() == 4 else (B,), torch.int32)
         where, flags = positions, flags | FLAG_TOKEN_POSITIONS
     if q_out is None:
         q_out = torch.empty_like(q)
     else:
-        _tensor("q's output", q_out, q, q.shape, q.dtype)
+        _tensor("q's output", q_out, device, q.shape, el)
     if k is None:
         _need(k_out is None, "an output for k, but no k")
     elif k_out is None:
         k_out = torch.empty_like(k)
     else:
-        _tensor("k's output", k_out, q, k.shape, q.dtype)
-    params = SlaRotaryParams(dtype, B, T, Hq, Hk, d, 2 * frequencies.numel(), flags, magnitude)
-    _run(call, q, ctypes.byref(params), q.data_ptr(), _ptr(k), frequencies.data_ptr(), _ptr(where), _ptr(cu_seqlens),
-         q_out.data_ptr(), _ptr(k_out))
+        _tensor("k's output", k_out, device, k.shape, el)
+    _run(call, q, _params(SlaRotaryParams, _element("q", el), B, T, Hq, Hk, d, 2 * pairs, flags, magnitude), q.data_ptr(),
+         _ptr(k), frequencies.data_ptr(), _ptr(where), _ptr(cu_seqlens), q_out.data_ptr(), _ptr(k_out))
     return q_out, k_out
 
 
@@ -1058,22 +1071,27 @@ def rotary_backward(dq_out, dk_out, frequencies, *, start=None, positions=None, 
 
 
 def _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major):
-    import torch
-
+    """The parameter block, and the shape of everything but x and dx."""
+    torch = sys.modules["torch"]
+    device, el, shape = x.get_device(), x.dtype, x.shape
     B, T, H, dv = _batch("x", x, cu_seqlens, head_major)
-    dtype = _element("x", x)
-    _tensor("x", x, x, x.shape, x.dtype)
-    shape = torch.Size((B, T, H, dv)) if head_major else x.shape  # of everything but x, dx
+    _tensor("x", x, device, shape, el)
+    flags = 0
+    if head_major:
+        shape, flags = torch.Size((B, T, H, dv)), FLAG_HEAD_MAJOR
     _need(gate in GATES, f"gate: unknown {gate!r}")
-    _need((g is not None) == (gate != "none"), f"gate {gate!r}: {'needs g' if g is None else 'takes no g'}")
     if g is not None:
-        _tensor("g", g, x, shape, x.dtype)
-    flags = FLAG_HEAD_MAJOR if head_major else 0
+        _need(gate != "none", "gate 'none' takes no g")
+        _tensor("g", g, device, shape, el)
+    else:
+        _need(gate == "none", f"gate {gate!r} needs g")
     if w is not None:
-        heads = w.dim() == 2
-        _tensor("w", w, x, (H, dv) if heads else (dv,), torch.float32)
-        flags |= FLAG_HEAD_WEIGHTS if heads else 0
-    return SlaNormGateParams(dtype, B, T, H, dv, GATES[gate], flags, eps), shape
+        if w.dim() == 2:
+            flags |= FLAG_HEAD_WEIGHTS
+            _tensor("w", w, device, (H, dv), torch.float32)
+        else:
+            _tensor("w", w, device, (dv,), torch.float32)
+    return (SlaNormGateParams, _element("x", el), B, T, H, dv, GATES[gate], flags, eps), shape
 
 
 def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None, head_major: bool = False, out=None):
@@ -1085,8 +1103,8 @@ def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None
     if out is None:
         out = x.new_empty(shape)
     else:
-        _tensor("out", out, x, shape, x.dtype)
-    _run(load_library().sla_norm_gate, x, ctypes.byref(params), x.data_ptr(), _ptr(g), _ptr(w), _ptr(cu_seqlens), out.data_ptr())
+        _tensor("out", out, x.get_device(), shape, x.dtype)
+    _run(load_library().sla_norm_gate, x, _params(*params), x.data_ptr(), _ptr(g), _ptr(w), _ptr(cu_seqlens), out.data_ptr())
     return out
 
 
@@ -1094,47 +1112,46 @@ def norm_gate_backward(x, g, w, dy, *, gate: str = "silu", eps: float = 1e-5, cu
                        workspace=None):
     """Gradients of ``norm_gate`` for the cotangent dy of y, as a dict of new tensors: dx like x, dg like g (or None), dw like w
     (or None).  ``workspace``: a tensor of sla_norm_gate_backward_workspace_bytes, else it is allocated here."""
-    import torch
-
+    torch = sys.modules["torch"]
     params, shape = _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major)
-    _tensor("dy", dy, x, shape, x.dtype)
+    _tensor("dy", dy, x.get_device(), shape, x.dtype)
     dx = torch.empty_like(x)
     dg = None if g is None else torch.empty_like(g)
     dw = None if w is None else torch.empty_like(w)
-    if workspace is None and dw is not None:
-        workspace = x.new_empty(max(sla_norm_gate_backward_workspace_bytes(params, cu_seqlens is not None), 16), dtype=torch.uint8)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _run(load_library().sla_norm_gate_backward, x, ctypes.byref(params), x.data_ptr(), _ptr(g), _ptr(w), dy.data_ptr(),
+    size = 0
+    if workspace is not None:
+        size = workspace.numel() * workspace.element_size()
+    elif dw is not None:
+        size = _workspace_size(*params, packed=cu_seqlens is not None)
+        workspace = x.new_empty(size, dtype=torch.uint8)
+    _run(load_library().sla_norm_gate_backward, x, _params(*params), x.data_ptr(), _ptr(g), _ptr(w), dy.data_ptr(),
          _ptr(cu_seqlens), dx.data_ptr(), _ptr(dg), _ptr(dw), _ptr(workspace), size)
     return {"dx": dx, "dg": dg, "dw": dw}
 
 
-def _join_args(x, of, w_after, channel_scale, w_before, scale, eps, cu_seqlens):
-    """Params for the stream x [..., D] and, where there are any, block tensors ``of`` {name: tensor}."""
-    import torch
-
-    _need(x.dim() >= 1, "x: expected [..., D]")
-    D = x.shape[-1]
-    x_dtype = dtype = _element("x", x)
-    _tensor("x", x, x, x.shape, x.dtype)
+def _join_args(x, of, w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype=None):
+    """The parameter block for the stream x [..., D] and the block tensors ``of`` ((name, tensor), ...), of one type: that of
+    y_dtype or of the stream where there are none."""
+    torch = sys.modules["torch"]
+    device, shape = x.get_device(), x.shape
+    _need(len(shape) >= 1, "x: expected [..., D]")
+    D = shape[-1]
+    _tensor("x", x, device, shape, x.dtype)
     kind = None
-    for name, t in of.items():
+    for name, t in of:
         if t is not None:
             kind = kind or t.dtype
-            dtype = _element(name, t)
-            _tensor(name, t, x, x.shape, kind)
+            _tensor(name, t, device, shape, kind)
     for name, t in (("w_after", w_after), ("channel_scale", channel_scale), ("w_before", w_before)):
         if t is not None:
-            _tensor(name, t, x, (D,), torch.float32)
+            _tensor(name, t, device, (D,), torch.float32)
     if cu_seqlens is not None:
-        _need(x.dim() == 2, "x: a packed batch is [T,D]")
-        _need(cu_seqlens.dtype is torch.int32 and cu_seqlens.dim() == 1 and cu_seqlens.numel() >= 1
-              and cu_seqlens.is_contiguous() and cu_seqlens.get_device() == x.get_device(),
-              f"cu_seqlens: expected a contiguous int32 tensor [B+1] on {x.device}")
-        return SlaJoinNormParams(dtype, x_dtype, cu_seqlens.numel() - 1, x.shape[0], D, scale, eps)
-    tokens = x.numel() // D if D else 0
-    _need(tokens < 1 << 31, f"x: {tuple(x.shape)} is out of range")
-    return SlaJoinNormParams(dtype, x_dtype, 1, tokens, D, scale, eps)
+        _need(len(shape) == 2, "x: a packed batch is [T,D]")
+        B, T = _sequences("x", cu_seqlens, device), shape[0]
+    else:
+        B, T = 1, x.numel() // D if D else 0
+    _need(T < 1 << 31 and D < 1 << 31, f"x: {tuple(shape)} is out of range")
+    return SlaJoinNormParams, _element("h", kind or y_dtype or x.dtype), _element("x", x.dtype), B, T, D, scale, eps
 
 
 def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float = 1.0, eps: float = 1e-5, cu_seqlens=None,
@@ -1143,21 +1160,19 @@ def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float 
     u = h, or h / rms(h) * w_after;  x_out = x + scale * channel_scale * u;  y = x_out / rms(x_out) * w_before.  x, h [..., D]
     ([T,D] with cu_seqlens), x float32 or of h's type; weights float32 [D].  Returns (x_out, y).  h None: no join, x_out is x, and
     y has y_dtype (default: x's type); w_before None: no norm, y is None.  ``x_out`` may be x and ``y`` may be h."""
-    import torch
-
+    torch = sys.modules["torch"]
     _need(h is not None or (w_before is not None and w_after is None and channel_scale is None and x_out is None),
           "h: needed, unless only the norm of x is asked for")
     _need(w_before is not None or y is None, "an output y, but no w_before")
-    params = _join_args(x, {"h": h, "y": y}, w_after, channel_scale, w_before, scale, eps, cu_seqlens)
+    params = _join_args(x, (("h", h), ("y", y)), w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype)
     if h is not None:
         if x_out is None:
             x_out = torch.empty_like(x)
         else:
-            _tensor("x_out", x_out, x, x.shape, x.dtype)
+            _tensor("x_out", x_out, x.get_device(), x.shape, x.dtype)
     if w_before is not None and y is None:
-        y = torch.empty_like(x, dtype=h.dtype if h is not None else y_dtype or x.dtype)
-        params.dtype = _element("y", y)
-    _run(load_library().sla_join_norm, x, ctypes.byref(params), x.data_ptr(), _ptr(h), _ptr(w_after), _ptr(channel_scale),
+        y = torch.empty_like(x, dtype=y_dtype) if h is None else torch.empty_like(h)
+    _run(load_library().sla_join_norm, x, _params(*params), x.data_ptr(), _ptr(h), _ptr(w_after), _ptr(channel_scale),
          _ptr(w_before), _ptr(cu_seqlens), _ptr(x_out), _ptr(y))
     return (x if h is None else x_out), y
 
@@ -1168,23 +1183,26 @@ def join_norm_backward(x_out, h, w_before, dy, dx_out=None, *, w_after=None, cha
     dx, dh, dw_after, dchannel_scale, dw_before (None where the forward had no such input).  Without w_before (and dy) dx is
     dx_out itself.  h is read only with w_after or channel_scale; None: the forward only normalised x.  ``workspace``: a tensor of
     sla_join_norm_backward_workspace_bytes, else it is allocated here."""
-    import torch
-
+    torch = sys.modules["torch"]
     _need((dy is None) == (w_before is None) and (dy is not None or dx_out is not None), "dy goes with w_before; without them dx_out")
     _need(h is not None or (w_after is None and channel_scale is None), "h: needed with w_after or channel_scale")
-    params = _join_args(x_out, {"dy": dy, "h": h}, w_after, channel_scale, w_before, scale, eps, cu_seqlens)
+    params = _join_args(x_out, (("dy", dy), ("h", h)), w_after, channel_scale, w_before, scale, eps, cu_seqlens)
     if dx_out is not None:
-        _tensor("dx_out", dx_out, x_out, x_out.shape, x_out.dtype)
-    like = lambda t: None if t is None else torch.empty_like(t)
-    dx = dx_out if dy is None else torch.empty_like(x_out)
-    g = {"dx": dx, "dh": like(h), "dw_after": like(w_after), "dchannel_scale": like(channel_scale), "dw_before": like(w_before)}
-    if dy is None and h is None:
-        return g
-    sums = dy is not None or w_after is not None or channel_scale is not None
-    if workspace is None and sums:
-        workspace = x_out.new_empty(max(sla_join_norm_backward_workspace_bytes(params, cu_seqlens is not None), 16), dtype=torch.uint8)
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _run(load_library().sla_join_norm_backward, x_out, ctypes.byref(params), x_out.data_ptr(), _ptr(h), _ptr(w_after),
-         _ptr(channel_scale), _ptr(w_before), _ptr(dy), _ptr(dx_out), _ptr(cu_seqlens), None if dy is None else dx.data_ptr(),
-         _ptr(g["dh"]), _ptr(g["dw_after"]), _ptr(g["dchannel_scale"]), _ptr(g["dw_before"]), _ptr(workspace), size)
-    return g
+        _tensor("dx_out", dx_out, x_out.get_device(), x_out.shape, x_out.dtype)
+    like = torch.empty_like
+    dx = dx_out if dy is None else like(x_out)
+    dh = None if h is None else like(h)
+    dw_after = None if w_after is None else like(w_after)
+    dchannel = None if channel_scale is None else like(channel_scale)
+    dw_before = None if w_before is None else like(w_before)
+    if dy is not None or h is not None:
+        size = 0
+        if workspace is not None:
+            size = workspace.numel() * workspace.element_size()
+        elif dy is not None or dw_after is not None or dchannel is not None:
+            size = _workspace_size(*params, packed=cu_seqlens is not None)
+            workspace = x_out.new_empty(size, dtype=torch.uint8)
+        _run(load_library().sla_join_norm_backward, x_out, _params(*params), x_out.data_ptr(), _ptr(h), _ptr(w_after),
+             _ptr(channel_scale), _ptr(w_before), _ptr(dy), _ptr(dx_out), _ptr(cu_seqlens), None if dy is None else dx.data_ptr(),
+             _ptr(dh), _ptr(dw_after), _ptr(dchannel), _ptr(dw_before), _ptr(workspace), size)
+    return {"dx": dx, "dh": dh, "dw_after": dw_after, "dchannel_scale": dchannel, "dw_before": dw_before}
