@@ -5,10 +5,13 @@
 // turned like this in front of the recurrence of Sec. 5.1; with a relative angle per token the products q . k see only the
 // distance between two tokens.
 //
-// A streaming pass: 3 flops an element.  The angles are made here instead of read from a table: a thread keeps its pairs'
-// frequencies, and the cosines of a token serve all of its heads that the thread walks.  An angle is reduced to a quarter
-// turn in fp64 (position * frequency / 2 pi minus its nearest multiple of 1/4: exact but for the product's rounding of
-// 2^-53), so far positions cost no accuracy; sine and cosine of what is left, |x| <= pi/4, are their Taylor polynomials.
+// A streaming pass of 3 flops an element, bound by memory.  Measured in bf16 (a large copy reaches 5.4 TB/s, more where the
+// last-level cache holds part of it): B=8 T=2048 16+16 heads of 128, 268 MB, 45 us; T=65536 32+32 heads, 2.1 GB, 397 us.
+//
+// The angles are made here instead of read from a table: a thread keeps its pairs' frequencies, and the cosines of a token
+// serve all of its heads that the thread walks.  An angle is reduced to a quarter turn in fp64 (position * frequency / 2 pi
+// minus its nearest multiple of 1/4: exact but for the product's rounding of 2^-53), so far positions cost no accuracy; sine
+// and cosine of what is left, |x| <= pi/4, are their Taylor polynomials.
 #include "sla_row_ops.h"
 
 namespace sla {
@@ -17,7 +20,7 @@ namespace {
 
 using namespace row_ops;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;    // a head takes at most 73 of them
 constexpr int kHeadsAhead = 4;  // heads whose loads a thread has in flight
 constexpr int kMaxHeads = 1024, kMaxWidth = 512;
 
@@ -70,12 +73,12 @@ __device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int64_t n) 
 }
 
 // ADJ: pairs (2i, 2i+1), a thread turns the four pairs of eight adjacent elements.  Otherwise pairs (i, i + r/2), a thread
-// turns V of them: eight where r/2 is a multiple of eight, so that both halves are read 16 bytes at a time, else one (2-byte
-// accesses, 64 adjacent ones a wave).  Elements from r on are copied, V (or eight) at a time; in place they stay.
-template <bool BF16, bool ADJ, int V>
-__global__ __launch_bounds__(512) void sla_rotary_kernel(RotaryArgs a) {
-    constexpr int P = ADJ ? 4 : V;  // pairs of a thread
-    const int turned = ADJ ? (a.r + 7) / 8 : a.r / 2 / V;
+// turns eight of them, or copies eight of the elements from r on.  ODD: r/2 is no multiple of eight, so the second half and what
+// is copied begin anywhere, and the last pairs and elements that make no eight have a thread each (bf16, B=4 T=2048 16+16 heads
+// of 128 with 100 elements turned: 30.6 us, 134 MB; a thread for every pair, 2 bytes at a time: 61 us).
+template <bool BF16, bool ADJ, bool ODD>
+__global__ __launch_bounds__(kThreads) void sla_rotary_kernel(RotaryArgs a) {
+    constexpr int P = ADJ ? 4 : 8;  // pairs of a thread
     int tl, hl, c;
     {
         const int x = threadIdx.x / a.pieces;
@@ -89,14 +92,36 @@ __global__ __launch_bounds__(512) void sla_rotary_kernel(RotaryArgs a) {
         }
     }
     if (tl >= a.tokens || hl >= a.head_lanes) return;
-    const bool turns = c < turned;
-    const int off0 = ADJ ? 8 * c : (turns ? V * c : a.r + V * (c - turned)), off1 = a.r / 2 + off0;
+    // the thread's first element, its pairs (0: it copies), and whether it has a single pair or element
+    int off, pairs;
+    bool single = false;
+    if (ADJ) {
+        off = 8 * c;
+        pairs = a.r / 2 - 4 * c;
+        pairs = pairs < 0 ? 0 : (pairs > 4 ? 4 : pairs);
+    } else {
+        const int half = a.r / 2, rest = a.d - a.r, wide = half / 8, wide_copies = rest / 8;
+        int q = c;
+        if (q < wide) {
+            off = 8 * q;
+            pairs = 8;
+        } else if ((q -= wide) < wide_copies) {
+            off = a.r + 8 * q;
+            pairs = 0;
+        } else if ((q -= wide_copies) < half % 8) {
+            off = 8 * wide + q;
+            pairs = 1;
+            single = true;
+        } else {
+            off = a.r + 8 * wide_copies + q - half % 8;
+            pairs = 0;
+            single = true;
+        }
+    }
+    const int off1 = off + a.r / 2;
     double f[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const int p = P * c + i;
-        f[i] = turns && p < a.r / 2 ? a.freq[p] * 0.15915494309189533577 : 0.0;
-    }
+    for (int i = 0; i < P; ++i) f[i] = i < pairs ? a.freq[(ADJ ? 4 * c : off) + i] * 0.15915494309189533577 : 0.0;
     int64_t first, end;
     token_range(a.cu, a.B, a.cu ? (int64_t)a.T : (int64_t)a.B * a.T, first, end);
     const int heads = a.Hq + a.Hk;
@@ -118,54 +143,69 @@ __global__ __launch_bounds__(512) void sla_rotary_kernel(RotaryArgs a) {
 #pragma unroll
         for (int i = 0; i < P; ++i) turn(pos * f[i], a.magnitude, a.sign, cs[i], sn[i]);
         for (int h0 = hl; h0 < heads; h0 += a.head_lanes * kHeadsAhead) {
-            float x[kHeadsAhead][8], y[kHeadsAhead][8];
-            const void* src[kHeadsAhead];
-            void* dst[kHeadsAhead];
-            size_t row[kHeadsAhead];
-#pragma unroll
-            for (int u = 0; u < kHeadsAhead; ++u) {
+            Raw8<BF16> rx[kHeadsAhead], ry[kHeadsAhead];
+            float x1[kHeadsAhead], y1[kHeadsAhead];
+            auto at = [&](int u, const void* q, const void* k, const void*& base) {  // the head's row in q or k
                 const int h = h0 + u * a.head_lanes;
-                if (h >= heads) break;
                 const bool isk = h >= a.Hq;
                 const int H = isk ? a.Hk : a.Hq, hh = isk ? h - a.Hq : h;
-                src[u] = isk ? a.k : a.q;
-                dst[u] = isk ? a.ko : a.qo;
-                row[u] = (a.head_major ? ((size_t)b * H + hh) * a.T + t : (size_t)n * H + hh) * a.d;
-                if constexpr (ADJ || V == 8) {
-                    load8<BF16>(src[u], row[u] + off0, x[u]);
-                    if (!ADJ && turns) load8<BF16>(src[u], row[u] + off1, y[u]);
+                base = isk ? k : q;
+                return (a.head_major ? ((size_t)b * H + hh) * a.T + t : (size_t)n * H + hh) * a.d;
+            };
+#pragma unroll
+            for (int u = 0; u < kHeadsAhead; ++u) {
+                if (h0 + u * a.head_lanes >= heads) break;
+                const void* src;
+                const size_t row = at(u, a.q, a.k, src);
+                if (ODD && single) {
+                    x1[u] = load1(src, row + off, BF16);
+                    if (pairs) y1[u] = load1(src, row + off1, BF16);
+                } else if constexpr (ODD) {
+                    fetch8_anywhere(src, row + off, rx[u]);
+                    if (pairs) fetch8_anywhere(src, row + off1, ry[u]);
                 } else {
-                    x[u][0] = load1(src[u], row[u] + off0, BF16);
-                    if (turns) y[u][0] = load1(src[u], row[u] + off1, BF16);
+                    fetch8(src, row + off, rx[u]);
+                    if (!ADJ && pairs) fetch8(src, row + off1, ry[u]);
                 }
             }
 #pragma unroll
             for (int u = 0; u < kHeadsAhead; ++u) {
                 if (h0 + u * a.head_lanes >= heads) break;
+                const void* to;
+                const size_t row = at(u, a.qo, a.ko, to);
+                void* dst = const_cast<void*>(to);
+                if (ODD && single) {
+                    const float e = x1[u], o = y1[u];
+                    store1(dst, row + off, pairs ? e * cs[0] - o * sn[0] : e, BF16);
+                    if (pairs) store1(dst, row + off1, e * sn[0] + o * cs[0], BF16);
+                    continue;
+                }
+                float x[8], y[8];
+                unpack8(rx[u], x);
                 if constexpr (ADJ) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float e = x[u][2 * i], o = x[u][2 * i + 1];
-                        const bool in = 4 * c + i < a.r / 2;
-                        x[u][2 * i] = in ? e * cs[i] - o * sn[i] : e;
-                        x[u][2 * i + 1] = in ? e * sn[i] + o * cs[i] : o;
+                        const float e = x[2 * i], o = x[2 * i + 1];
+                        x[2 * i] = i < pairs ? e * cs[i] - o * sn[i] : e;
+                        x[2 * i + 1] = i < pairs ? e * sn[i] + o * cs[i] : o;
                     }
-                    store8<BF16>(dst[u], row[u] + off0, x[u]);
+                    store8<BF16>(dst, row + off, x);
                 } else {
-                    if (turns) {
+                    if (pairs) {
+                        unpack8(ry[u], y);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            const float e = x[u][i], o = y[u][i];
-                            x[u][i] = e * cs[i] - o * sn[i];
-                            y[u][i] = e * sn[i] + o * cs[i];
+                        for (int i = 0; i < 8; ++i) {
+                            const float e = x[i], o = y[i];
+                            x[i] = e * cs[i] - o * sn[i];
+                            y[i] = e * sn[i] + o * cs[i];
                         }
                     }
-                    if constexpr (V == 8) {
-                        store8<BF16>(dst[u], row[u] + off0, x[u]);
-                        if (turns) store8<BF16>(dst[u], row[u] + off1, y[u]);
+                    if constexpr (ODD) {
+                        store8_anywhere<BF16>(dst, row + off, x);
+                        if (pairs) store8_anywhere<BF16>(dst, row + off1, y);
                     } else {
-                        store1(dst[u], row[u] + off0, x[u][0], BF16);
-                        if (turns) store1(dst[u], row[u] + off1, y[u][0], BF16);
+                        store8<BF16>(dst, row + off, x);
+                        if (pairs) store8<BF16>(dst, row + off1, y);
                     }
                 }
             }
@@ -199,28 +239,31 @@ int rotary(const sla_rotary_params* p, const void* q, const void* k, const doubl
     if (rc != SLA_OK) return rc;
     if (p->B == 0 || p->T == 0) return SLA_OK;
     const bool adj = p->flags & SLA_FLAG_ADJACENT_PAIRS;
-    const bool wide = adj || p->rotary % 16 == 0;
+    const int half = p->rotary / 2, rest = p->d - p->rotary;
+    const bool odd = !adj && half % 8 != 0;
     RotaryArgs a{q, k, qo, ko, freq, positions, cu, p->B, p->T, p->Hq, p->Hk, p->d, p->rotary};
     a.per_token = (p->flags & SLA_FLAG_TOKEN_POSITIONS) != 0;
     a.head_major = (p->flags & SLA_FLAG_HEAD_MAJOR) != 0;
     a.magnitude = p->magnitude;
     a.sign = sign;
-    a.pieces = adj ? p->d / 8 : (wide ? p->rotary / 16 + (p->d - p->rotary) / 8 : p->d - p->rotary / 2);
+    a.pieces = adj ? p->d / 8 : half / 8 + rest / 8 + half % 8 + rest % 8;  
     const int64_t tokens = cu ? p->T : (int64_t)p->B * p->T;
     const int heads = p->Hq + p->Hk;
-    const int threads = a.pieces > kThreads ? 512 : kThreads;
-    int each = kHeadsAhead;  // heads a thread walks: fewer while that leaves compute units without work
+    // Heads a thread walks: their turns share one set of angles.  bf16, B=8 T=2048 16+16 heads of 128: 2, 4, 8, 16, 32 heads
+    // 57.1, 48.0, 45.3, 55.0, 55.1 us, head-major 64.4, 51.1, 46.9, 44.9, 45.0 us; B=4 T=4096 32+4 heads 85.5, 56.1, 54.1,
+    // 55.1, 59.4 us.  Fewer while that leaves less than two waves a SIMD.
+    int each = 8;
     while (each > 1 && tokens * a.pieces * ((heads + each - 1) / each) < (int64_t)kComputeUnits * 512) each /= 2;
     a.head_lanes = (heads + each - 1) / each;
-    if (a.head_lanes * a.pieces > threads) a.head_lanes = threads / a.pieces;
-    a.tokens = threads / (a.head_lanes * a.pieces);
+    if (a.head_lanes * a.pieces > kThreads) a.head_lanes = kThreads / a.pieces;
+    a.tokens = kThreads / (a.head_lanes * a.pieces);
     const int64_t blocks = (tokens + a.tokens - 1) / a.tokens;
     const dim3 grid((unsigned)(blocks < kComputeUnits * 64 ? blocks : kComputeUnits * 64));
-#define SLA_ROT(BF, ADJ, V) hipLaunchKernelGGL((sla_rotary_kernel<BF, ADJ, V>), grid, dim3(threads), 0, stream, a)
+#define SLA_ROT(BF, ADJ, ODD) hipLaunchKernelGGL((sla_rotary_kernel<BF, ADJ, ODD>), grid, dim3(kThreads), 0, stream, a)
     if (p->dtype == SLA_BF16) {
-        if (adj) SLA_ROT(true, true, 8); else if (wide) SLA_ROT(true, false, 8); else SLA_ROT(true, false, 1);
+        if (adj) SLA_ROT(true, true, false); else if (odd) SLA_ROT(true, false, true); else SLA_ROT(true, false, false);
     } else {
-        if (adj) SLA_ROT(false, true, 8); else if (wide) SLA_ROT(false, false, 8); else SLA_ROT(false, false, 1);
+        if (adj) SLA_ROT(false, true, false); else if (odd) SLA_ROT(false, false, true); else SLA_ROT(false, false, false);
     }
 #undef SLA_ROT
     return hipGetLastError() == hipSuccess ? SLA_OK : SLA_ERR_HIP;
