@@ -20,6 +20,7 @@ namespace {
 using namespace row_ops;
 
 constexpr int kMaxWidth = 16384;
+constexpr int kForwardWaves = 4, kBackwardWaves = 8;  // of a workgroup, where a row takes no more
 
 struct JoinArgs {
     const void *x, *h, *dy, *dxo;
@@ -127,37 +128,55 @@ __global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
     }
 }
 
-// With V == 1 the vectors of weights stay in registers and the next row's loads are under way while a row is worked on; with more
-// (rows over 4096, up to 1024 threads) there are no registers for either.
-template <bool XBF, bool HBF, int V>
-__global__ __launch_bounds__(V == 1 ? 512 : 1024) void sla_join_norm_backward_kernel(JoinArgs a) {
-    extern __shared__ float red[];  // the exchange buffer; after it [rows - 1][planes][row_waves * 64 * 8 * V] sums
+// Adds eight sums to those in LDS that the thread keeps there, and clears them.
+__device__ __forceinline__ void add_to(float* at, float (&f)[8]) {
+    float u[8];
+    load8<false>(at, 0, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        u[i] += f[i];
+        f[i] = 0.f;
+    }
+    store8<false>(at, 0, u);
+}
+
+// Rows up to 4096 (THREADS 512): the weights stay in registers, and the next row's loads are under way while a row is worked on.
+// Up to 8192 (THREADS 1024) the registers hold the weights, beyond that (V = 2) neither: the sums over tokens move to LDS too.
+template <bool XBF, bool HBF, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArgs a) {
+    extern __shared__ float red[];  // the exchange buffer; after it [V == 1 ? rows - 1 : 1][planes][row_waves * 64 * 8 * V] sums
+    constexpr bool kAhead = THREADS == 512;
+    float* lds = red + 2 * 16 * 4;
     int flip = 0;
     const int wv = threadIdx.x >> 6, slot = wv / a.row_waves;
     const int col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8;
     const bool reads_h = a.w_after || a.channel;
+    const int planes = reads_h ? 2 : 1, width = next * V;
     Raw8<XBF> x_[V], dxo_[V];
     Raw8<HBF> dy_[V], h_[V];
-    float wb[V][8], cw[V][8], pw[V][8], pp[V][8];
-    // w_before (0 without dy) and scale * channel * w_after at column j; past the row's end nothing is read
-    auto weights = [&](int v, int j) {
-        float w[8];
+    float wb[8], cw[8], pw[8], pp[8];
+    // w_before (0 without dy), and scale * channel * w_after, at piece v; past the row's end nothing is read
+    auto before = [&](int v, float (&w)[8]) {
+        const int j = col + v * next;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            wb[v][i] = 0.f;
-            cw[v][i] = a.scale;
-        }
+        for (int i = 0; i < 8; ++i) w[i] = 0.f;
+        if (a.dy && j < a.D) load8<false>(a.w_before, j, w);
+    };
+    auto after = [&](int v, float (&w)[8]) {
+        const int j = col + v * next;
+        float u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = a.scale;
         if (j >= a.D) return;
-        if (a.dy) load8<false>(a.w_before, j, wb[v]);
         if (a.w_after) {
-            load8<false>(a.w_after, j, w);
+            load8<false>(a.w_after, j, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) cw[v][i] *= w[i];
+            for (int i = 0; i < 8; ++i) w[i] *= u[i];
         }
         if (a.channel) {
-            load8<false>(a.channel, j, w);
+            load8<false>(a.channel, j, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) cw[v][i] *= w[i];
+            for (int i = 0; i < 8; ++i) w[i] *= u[i];
         }
     };
     auto fetch = [&](int64_t n) {
@@ -175,41 +194,51 @@ __global__ __launch_bounds__(V == 1 ? 512 : 1024) void sla_join_norm_backward_ke
         }
     };
 #pragma unroll
+    for (int i = 0; i < 8; ++i) pw[i] = pp[i] = 0.f;
+    if (V == 1) {
+        before(0, wb);
+        after(0, cw);
+    }
+#pragma unroll
     for (int v = 0; v < V; ++v) {
         x_[v] = {}; dxo_[v] = {}; dy_[v] = {}; h_[v] = {};  // what is never fetched counts as zero
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pw[v][i] = pp[v][i] = 0.f;
-        if (V == 1) weights(v, col + v * next);
+        if (V > 1 && a.part) {
+            store8<false>(lds, col + v * next, pw);
+            if (reads_h) store8<false>(lds, width + col + v * next, pp);
+        }
     }
     int64_t first, end;
     token_range(a.cu, a.B, a.tokens, first, end);
     const int64_t step = (int64_t)gridDim.x * a.rows;
     int64_t r0 = first + (int64_t)blockIdx.x * a.rows;
-    if (V == 1 && r0 + slot < end) fetch(r0 + slot);
+    if (kAhead && r0 + slot < end) fetch(r0 + slot);
     for (; r0 < end; r0 += step) {
         const int64_t n = r0 + slot;
         const size_t row = (size_t)n * a.D;
         const bool there = n < end;  // where not, the lanes hold some other row: nothing of it is stored or summed
-        if (V > 1 && there) fetch(n);
-        float x[V][8], dy[V][8], dx[V][8], h[V][8];
+        if (!kAhead && there) fetch(n);
+        float dx[V][8], h[V][8];
+        float s[3] = {0.f, 0.f, 0.f};
+        Raw8<XBF> xr[V];
+        Raw8<HBF> yr[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if (V > 1) weights(v, col + v * next);
-            unpack8(x_[v], x[v]);
-            unpack8(dy_[v], dy[v]);
+            float x[8], dy[8];
+            if (V > 1) before(v, wb);
+            xr[v] = x_[v];
+            yr[v] = dy_[v];
+            unpack8(xr[v], x);
+            unpack8(yr[v], dy);
             unpack8(dxo_[v], dx[v]);
             unpack8(h_[v], h[v]);
-        }
-        if (V == 1 && n + step < end) fetch(n + step);
-        float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-        for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                s[0] += x[v][i] * x[v][i];
-                s[1] += dy[v][i] * wb[v][i] * x[v][i];
+                s[0] += x[i] * x[i];
+                s[1] += dy[i] * wb[i] * x[i];
                 s[2] += h[v][i] * h[v][i];
             }
+        }
+        if (kAhead && n + step < end) fetch(n + step);
         row_sums(s, a.row_waves, red, flip);
         const float rh = a.w_after ? inverse_root(s[2] * a.inv_d + a.eps) : 1.f;
         if (a.dy) {
@@ -217,12 +246,17 @@ __global__ __launch_bounds__(V == 1 ? 512 : 1024) void sla_join_norm_backward_ke
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int j = col + v * next;
+                float x[8], dy[8];
+                if (V > 1) before(v, wb);
+                unpack8(xr[v], x);
+                unpack8(yr[v], dy);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float n_ = x[v][i] * r;
-                    if (there) pw[v][i] += dy[v][i] * n_;
-                    dx[v][i] += r * (dy[v][i] * wb[v][i] - n_ * mean);
+                    const float n_ = x[i] * r;
+                    if (there) pw[i] += dy[i] * n_;
+                    dx[v][i] += r * (dy[i] * wb[i] - n_ * mean);
                 }
+                if (V > 1 && a.part) add_to(lds + j, pw);
                 if (j < a.D && there) store8<XBF>(a.dx, row + j, dx[v]);
             }
         }
@@ -230,13 +264,15 @@ __global__ __launch_bounds__(V == 1 ? 512 : 1024) void sla_join_norm_backward_ke
         float t[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            if (V > 1) after(v, cw);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 h[v][i] *= rh;
-                if (there) pp[v][i] += dx[v][i] * h[v][i];
-                dx[v][i] *= cw[v][i];
+                if (there) pp[i] += dx[v][i] * h[v][i];
+                dx[v][i] *= cw[i];
                 t[0] += dx[v][i] * h[v][i];
             }
+            if (V > 1 && a.part && reads_h) add_to(lds + width + col + v * next, pp);
         }
         if (a.w_after) row_sums(t, a.row_waves, red, flip);
         const float mean = a.w_after ? t[0] * a.inv_d : 0.f;
@@ -250,37 +286,37 @@ __global__ __launch_bounds__(V == 1 ? 512 : 1024) void sla_join_norm_backward_ke
     }
     if (!a.part) return;
     // one partial sum a workgroup: the rows beside the first leave theirs in LDS
-    float* lds = red + 2 * 16 * 4;
-    const int planes = reads_h ? 2 : 1, width = next * V;
-    if (slot > 0) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            store8<false>(lds, (size_t)(slot - 1) * planes * width + col + v * next, pw[v]);
-            if (planes == 2) store8<false>(lds, (size_t)((slot - 1) * planes + 1) * width + col + v * next, pp[v]);
-        }
+    if (V == 1 && slot > 0) {
+        store8<false>(lds, (size_t)(slot - 1) * planes * width + col, pw);
+        if (planes == 2) store8<false>(lds, (size_t)((slot - 1) * planes + 1) * width + col, pp);
     }
     __syncthreads();
     if (slot > 0) return;
     float* out = a.part + (size_t)blockIdx.x * planes * a.D;
+    const int others = V == 1 ? a.rows - 1 : 1;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int j = col + v * next;
         if (j >= a.D) continue;
-        for (int q = 0; q < a.rows - 1; ++q) {
-            float u[8];
+        float u[8];
+        if (V > 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pw[i] = pp[i] = 0.f;
+        }
+        for (int q = 0; q < others; ++q) {
             load8<false>(lds, (size_t)q * planes * width + j, u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pw[v][i] += u[i];
+            for (int i = 0; i < 8; ++i) pw[i] += u[i];
             if (planes == 2) {
                 load8<false>(lds, (size_t)(q * planes + 1) * width + j, u);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) pp[v][i] += u[i];
+                for (int i = 0; i < 8; ++i) pp[i] += u[i];
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pp[v][i] *= a.scale;
-        store8<false>(out, j, pw[v]);
-        if (planes == 2) store8<false>(out, a.D + j, pp[v]);
+        for (int i = 0; i < 8; ++i) pp[i] *= a.scale;
+        store8<false>(out, j, pw);
+        if (planes == 2) store8<false>(out, a.D + j, pp);
     }
 }
 
@@ -325,43 +361,31 @@ int check_join(const sla_join_norm_params* p, const int32_t* cu) {
 
 int64_t tokens_of(const sla_join_norm_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
 
-// How a row lies over lanes: v pieces of eight a lane.  Four rows of a wave each as long as that takes at most `most` pieces,
-// else more waves a row.
+// How a row lies over lanes: one piece of eight a lane and as many waves as that takes, or two pieces in rows over 8192.  More rows share a workgroup of `waves` waves where theirs leave room.
 struct Split {
     int v, row_waves, rows, threads;
 };
-Split split(int D, int most) {
-    Split s{1, 1, 1, 256};
-    while (s.row_waves < 16 && s.row_waves * 64 * 8 * most < D) s.row_waves *= 2;
-    while (s.row_waves * 64 * 8 * s.v < D) s.v *= 2;
-    s.rows = s.row_waves < 4 ? 4 / s.row_waves : 1;
-    s.threads = s.row_waves < 4 ? 256 : s.row_waves * 64;
+Split split(int D, int waves) {
+    Split s{1, 1, 1, 64 * waves};
+    while (s.row_waves < 16 && s.row_waves * 64 * 8 < D) s.row_waves *= 2;
+    if (s.row_waves * 64 * 8 < D) s.v = 2;
+    if (s.row_waves < waves) s.rows = waves / s.row_waves; else s.threads = 64 * s.row_waves;
     return s;
 }
 
-Split forward_split(int D, int64_t tokens) {
-    Split s = split(D, 4);
-    if (tokens * s.row_waves < (int64_t)kComputeUnits * 8) s = split(D, 1);  // few rows: as many lanes on each as there are pieces
-    return s;
+// Launches with more than the 64 KB of LDS that a kernel gets without asking.
+template <typename F>
+bool allow_lds(F kernel, size_t lds) {
+    if (lds <= 64 * 1024 || hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess)
+        return true;
+    (void)hipGetLastError();
+    return false;
 }
 
-// The backward's: one piece a lane up to 4096 columns, and eight waves a workgroup (sixteen where a row takes them).
-Split backward_split(int D) {
-    Split s{1, 1, 1, 512};
-    while (s.row_waves < 8 && s.row_waves * 64 * 8 < D) s.row_waves *= 2;
-    if (s.row_waves * 64 * 8 < D) {
-        s.v = 2;
-        if (s.row_waves * 64 * 8 * 2 < D) s.row_waves = 16;
-    }
-    s.rows = s.row_waves < 8 ? 8 / s.row_waves : 1;
-    if (s.row_waves == 16) s.threads = 1024;
-    return s;
-}
-
-constexpr int64_t kBackwardGroups = kComputeUnits * 2;  // workgroups, and with them partial sums
+// Workgroups of the backward, each of which leaves a partial sum: as many as are at work at a time.
 unsigned backward_workgroups(const Split& s, int64_t tokens) {
-    const int64_t n = (tokens + s.rows - 1) / s.rows;
-    return (unsigned)(n < kBackwardGroups ? n : kBackwardGroups);
+    const int64_t n = (tokens + s.rows - 1) / s.rows, most = kComputeUnits * (s.threads == 1024 ? 1 : 2);
+    return (unsigned)(n < most ? n : most);
 }
 
 }  // namespace
@@ -395,13 +419,13 @@ int sla_join_norm(const sla_join_norm_params* p, const void* x, const void* h, c
     a.x = x; a.h = h; a.w_after = w_after; a.channel = channel_scale; a.w_before = w_before; a.xo = x_out; a.y = y;
     a.cu = cu_seqlens; a.tokens = tokens_of(*p, cu_seqlens); a.B = p->B; a.D = p->D;
     a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.f / p->D;
-    const Split s = forward_split(p->D, a.tokens);
+    const Split s = split(p->D, kForwardWaves);
     a.row_waves = s.row_waves; a.rows = s.rows;
     const int64_t blocks = (a.tokens + s.rows - 1) / s.rows;
     const dim3 grid((unsigned)(blocks < kComputeUnits * 64 ? blocks : kComputeUnits * 64));
 #define SLA_JN(X, Y, V) hipLaunchKernelGGL((sla_join_norm_kernel<X, Y, V>), grid, dim3(s.threads), 0, (hipStream_t)stream, a)
 #define SLA_JN_V(X, Y) \
-    if (s.v == 1) SLA_JN(X, Y, 1); else if (s.v == 2) SLA_JN(X, Y, 2); else SLA_JN(X, Y, 4)
+    if (s.v == 1) SLA_JN(X, Y, 1); else SLA_JN(X, Y, 2)
     if (p->dtype == SLA_F32) { SLA_JN_V(false, false); }
     else if (p->x_dtype == SLA_F32) { SLA_JN_V(false, true); }
     else { SLA_JN_V(true, true); }
@@ -413,7 +437,7 @@ int sla_join_norm(const sla_join_norm_params* p, const void* x, const void* h, c
 size_t sla_join_norm_backward_workspace_bytes(const sla_join_norm_params* p, int packed) {
     using namespace sla;
     if (check_join(p, nullptr) != SLA_OK || p->B == 0 || p->T == 0) return 0;
-    return (size_t)backward_workgroups(backward_split(p->D), tokens_of(*p, packed)) * 2 * p->D * sizeof(float);
+    return (size_t)backward_workgroups(split(p->D, kBackwardWaves), tokens_of(*p, packed)) * 2 * p->D * sizeof(float);
 }
 
 int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, const void* h, const float* w_after,
@@ -446,14 +470,18 @@ int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, con
     a.dx = dx; a.dh = dh; a.part = sums ? (float*)workspace : nullptr;
     a.cu = cu_seqlens; a.tokens = tokens_of(*p, cu_seqlens); a.B = p->B; a.D = p->D;
     a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.f / p->D;
-    const Split s = backward_split(p->D);
+    const Split s = split(p->D, kBackwardWaves);
     a.row_waves = s.row_waves; a.rows = s.rows;
     const unsigned blocks = backward_workgroups(s, a.tokens);
-    const size_t lds = (2 * 16 * 4 + (size_t)(s.rows - 1) * planes * s.row_waves * 64 * 8 * s.v) * sizeof(float);
-#define SLA_JN(X, Y, V) \
-    hipLaunchKernelGGL((sla_join_norm_backward_kernel<X, Y, V>), dim3(blocks), dim3(s.threads), lds, (hipStream_t)stream, a)
+    const size_t lds = (2 * 16 * 4 + (size_t)(s.v == 1 ? s.rows - 1 : 1) * planes * s.row_waves * 64 * 8 * s.v) * sizeof(float);
+#define SLA_JN(X, Y, V, N)                                                                                              \
+    do {                                                                                                                \
+        const auto kernel = sla_join_norm_backward_kernel<X, Y, V, N>;                                                    \
+        if (!allow_lds(kernel, lds)) return SLA_ERR_HIP;                                                                 \
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(s.threads), lds, (hipStream_t)stream, a);                          \
+    } while (0)
 #define SLA_JN_V(X, Y) \
-    if (s.v == 1) SLA_JN(X, Y, 1); else SLA_JN(X, Y, 2)
+    if (s.v == 2) SLA_JN(X, Y, 2, 1024); else if (s.threads == 1024) SLA_JN(X, Y, 1, 1024); else SLA_JN(X, Y, 1, 512)
     if (p->dtype == SLA_F32) { SLA_JN_V(false, false); }
     else if (p->x_dtype == SLA_F32) { SLA_JN_V(false, true); }
     else { SLA_JN_V(true, true); }
