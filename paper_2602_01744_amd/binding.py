@@ -945,12 +945,13 @@ def _workspace_size(kind, *fields, packed):
 
 def _run(call, t, *args):
     """One call of the library on the current stream of t's device, with that device the current one; raises on a status."""
-    stream = _stream(t)
-    torch = sys.modules["torch"]
-    if torch._C._cuda_getDevice() == t.get_device():
-        rc = call(*args, stream)
+    c = sys.modules["torch"]._C
+    device = t.get_device()
+    if device >= 0 and device == c._cuda_getDevice():
+        rc = call(*args, c._cuda_getCurrentRawStream(device))
     else:
-        with torch.cuda.device(t.device):
+        stream = _stream(t)
+        with sys.modules["torch"].cuda.device(device):
             rc = call(*args, stream)
     if rc != 0:
         raise SlaError(rc, sla_status_string(rc))
@@ -973,19 +974,24 @@ def _sequences(name, cu_seqlens, device):
 
 
 def _batch(name, t, cu_seqlens, head_major):
-    """(B, T, H, width) of a tensor of head vectors: [B,T,H,d] ([B,H,T,d] head-major); [T,H,d] with cu_seqlens; [B,H,d]
-    without: one token of each of B sequences, as decode_step has them."""
+    """(B, T, H, width) of a contiguous tensor of head vectors: [B,T,H,d] ([B,H,T,d] head-major); [T,H,d] with cu_seqlens;
+    [B,H,d] without: one token of each of B sequences, as decode_step has them."""
     shape = t.shape
     if cu_seqlens is not None:
         _need(len(shape) == 3 and not head_major, f"{name}: a packed batch is [T,H,d]")
-        sizes = (_sequences(name, cu_seqlens, t.get_device()), *shape)
+        B = _sequences(name, cu_seqlens, t.get_device())
+        T, H, d = shape
     elif len(shape) == 4:
-        sizes = (shape[0], shape[2], shape[1], shape[3]) if head_major else tuple(shape)
+        B, T, H, d = shape
+        if head_major:
+            T, H = H, T
     else:
         _need(len(shape) == 3 and not head_major, f"{name}: expected [B,T,H,d], [T,H,d] with cu_seqlens or [B,H,d]")
-        sizes = (shape[0], 1, shape[1], shape[2])
-    _need(max(sizes) < 1 << 31, f"{name}: {tuple(shape)} is out of range")
-    return sizes
+        B, H, d = shape
+        T = 1
+    if (B | T | H | d) >> 31 or not t.is_contiguous():
+        raise ValueError(f"{name}: {tuple(shape)} with strides {t.stride()} is not contiguous or out of range")
+    return B, T, H, d
 
 
 def rotary_frequencies(width: int, base: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
@@ -1022,11 +1028,10 @@ def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, mag
     torch = sys.modules["torch"]
     device, el, Hk = q.get_device(), q.dtype, 0
     B, T, Hq, d = _batch("q", q, cu_seqlens, head_major)
-    _tensor("q", q, device, q.shape, el)
     if k is not None:
-        Bk, Tk, Hk, dk = _batch("k", k, cu_seqlens, head_major) if k.shape != q.shape else (B, T, Hq, d)
-        _need(Bk == B and Tk == T and dk == d, f"k: {tuple(k.shape)} does not go with q: {tuple(q.shape)}")
-        _tensor("k", k, device, k.shape, el)
+        Bk, Tk, Hk, dk = _batch("k", k, cu_seqlens, head_major)
+        if Bk != B or Tk != T or dk != d or k.dtype is not el or k.get_device() != device:
+            raise ValueError(f"k: {k.dtype} {tuple(k.shape)} on {k.device} does not go with q: {el} {tuple(q.shape)} on {q.device}")
     pairs = frequencies.numel()
     _tensor("frequencies", frequencies, device, (pairs,), torch.float64)
     flags = (FLAG_HEAD_MAJOR if head_major else 0) | (FLAG_ADJACENT_PAIRS if adjacent else 0)
@@ -1075,7 +1080,6 @@ def _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major):
     torch = sys.modules["torch"]
     device, el, shape = x.get_device(), x.dtype, x.shape
     B, T, H, dv = _batch("x", x, cu_seqlens, head_major)
-    _tensor("x", x, device, shape, el)
     flags = 0
     if head_major:
         shape, flags = torch.Size((B, T, H, dv)), FLAG_HEAD_MAJOR
@@ -1101,7 +1105,7 @@ def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None
     head_major, x."""
     params, shape = _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major)
     if out is None:
-        out = x.new_empty(shape)
+        out = x.new_empty(shape) if head_major else sys.modules["torch"].empty_like(x)
     else:
         _tensor("out", out, x.get_device(), shape, x.dtype)
     _run(load_library().sla_norm_gate, x, _params(*params), x.data_ptr(), _ptr(g), _ptr(w), _ptr(cu_seqlens), out.data_ptr())
@@ -1129,29 +1133,36 @@ def norm_gate_backward(x, g, w, dy, *, gate: str = "silu", eps: float = 1e-5, cu
     return {"dx": dx, "dg": dg, "dw": dw}
 
 
-def _join_args(x, of, w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype=None):
-    """The parameter block for the stream x [..., D] and the block tensors ``of`` ((name, tensor), ...), of one type: that of
-    y_dtype or of the stream where there are none."""
+def _join_args(x, one, other, w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype=None):
+    """The parameter block for the stream x [..., D] and the block's tensors ``one`` and ``other``, of one type: that of y_dtype or of
+    the stream where there are none."""
     torch = sys.modules["torch"]
-    device, shape = x.get_device(), x.shape
-    _need(len(shape) >= 1, "x: expected [..., D]")
+    device, shape, el = x.get_device(), x.shape, x.dtype
+    _need(len(shape) >= 1 and x.is_contiguous(), "x: expected a contiguous tensor [..., D]")
     D = shape[-1]
-    _tensor("x", x, device, shape, x.dtype)
-    kind = None
-    for name, t in of:
-        if t is not None:
-            kind = kind or t.dtype
-            _tensor(name, t, device, shape, kind)
-    for name, t in (("w_after", w_after), ("channel_scale", channel_scale), ("w_before", w_before)):
-        if t is not None:
-            _tensor(name, t, device, (D,), torch.float32)
+    kind = y_dtype or el
+    if one is not None:
+        kind = one.dtype
+        _tensor("h or dy", one, device, shape, kind)
+        if other is not None:
+            _tensor("h or y", other, device, shape, kind)
+    elif other is not None:
+        kind = other.dtype
+        _tensor("h or y", other, device, shape, kind)
+    if w_before is not None:
+        _tensor("w_before", w_before, device, (D,), torch.float32)
+    if w_after is not None:
+        _tensor("w_after", w_after, device, (D,), torch.float32)
+    if channel_scale is not None:
+        _tensor("channel_scale", channel_scale, device, (D,), torch.float32)
     if cu_seqlens is not None:
         _need(len(shape) == 2, "x: a packed batch is [T,D]")
         B, T = _sequences("x", cu_seqlens, device), shape[0]
     else:
         B, T = 1, x.numel() // D if D else 0
-    _need(T < 1 << 31 and D < 1 << 31, f"x: {tuple(shape)} is out of range")
-    return SlaJoinNormParams, _element("h", kind or y_dtype or x.dtype), _element("x", x.dtype), B, T, D, scale, eps
+    if (T | D) >> 31:
+        raise ValueError(f"x: {tuple(shape)} is out of range")
+    return SlaJoinNormParams, _element("h", kind), _element("x", el), B, T, D, scale, eps
 
 
 def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float = 1.0, eps: float = 1e-5, cu_seqlens=None,
@@ -1161,10 +1172,11 @@ def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float 
     ([T,D] with cu_seqlens), x float32 or of h's type; weights float32 [D].  Returns (x_out, y).  h None: no join, x_out is x, and
     y has y_dtype (default: x's type); w_before None: no norm, y is None.  ``x_out`` may be x and ``y`` may be h."""
     torch = sys.modules["torch"]
-    _need(h is not None or (w_before is not None and w_after is None and channel_scale is None and x_out is None),
-          "h: needed, unless only the norm of x is asked for")
+    if h is None:
+        _need(w_before is not None and w_after is None and channel_scale is None and x_out is None,
+              "h: needed, unless only the norm of x is asked for")
     _need(w_before is not None or y is None, "an output y, but no w_before")
-    params = _join_args(x, (("h", h), ("y", y)), w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype)
+    params = _join_args(x, h, y, w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype)
     if h is not None:
         if x_out is None:
             x_out = torch.empty_like(x)
@@ -1186,7 +1198,7 @@ def join_norm_backward(x_out, h, w_before, dy, dx_out=None, *, w_after=None, cha
     torch = sys.modules["torch"]
     _need((dy is None) == (w_before is None) and (dy is not None or dx_out is not None), "dy goes with w_before; without them dx_out")
     _need(h is not None or (w_after is None and channel_scale is None), "h: needed with w_after or channel_scale")
-    params = _join_args(x_out, (("dy", dy), ("h", h)), w_after, channel_scale, w_before, scale, eps, cu_seqlens)
+    params = _join_args(x_out, dy, h, w_after, channel_scale, w_before, scale, eps, cu_seqlens)
     if dx_out is not None:
         _tensor("dx_out", dx_out, x_out.get_device(), x_out.shape, x_out.dtype)
     like = torch.empty_like
