@@ -943,6 +943,11 @@ def _workspace_size(kind, *fields, packed):
     return max(query(kind(*fields), packed), 16)
 
 
+def _workspace_bytes(workspace, like):
+    _need(workspace.is_contiguous() and workspace.get_device() == like.get_device(), f"workspace: expected contiguous memory on {like.device}")
+    return workspace.numel() * workspace.element_size()
+
+
 def _run(call, t, *args):
     """One call of the library on the current stream of t's device, with that device the current one; raises on a status."""
     c = sys.modules["torch"]._C
@@ -1052,6 +1057,8 @@ def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, mag
         k_out = torch.empty_like(k)
     else:
         _tensor("k's output", k_out, device, k.shape, el)
+    if k is not None and (q_out.data_ptr() == k.data_ptr() or k_out.data_ptr() in (q.data_ptr(), q_out.data_ptr())) and q.numel():
+        raise ValueError("an output may lie on its own input only")
     _run(call, q, _params(SlaRotaryParams, _element("q", el), B, T, Hq, Hk, d, 2 * pairs, flags, magnitude), q.data_ptr(),
          _ptr(k), frequencies.data_ptr(), _ptr(where), _ptr(cu_seqlens), q_out.data_ptr(), _ptr(k_out))
     return q_out, k_out
@@ -1108,6 +1115,7 @@ def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None
         out = x.new_empty(shape) if head_major else sys.modules["torch"].empty_like(x)
     else:
         _tensor("out", out, x.get_device(), shape, x.dtype)
+        _need(not head_major or out.data_ptr() != x.data_ptr() or not x.numel(), "out may not be x, which is laid out differently")
     _run(load_library().sla_norm_gate, x, _params(*params), x.data_ptr(), _ptr(g), _ptr(w), _ptr(cu_seqlens), out.data_ptr())
     return out
 
@@ -1124,7 +1132,7 @@ def norm_gate_backward(x, g, w, dy, *, gate: str = "silu", eps: float = 1e-5, cu
     dw = None if w is None else torch.empty_like(w)
     size = 0
     if workspace is not None:
-        size = workspace.numel() * workspace.element_size()
+        size = _workspace_bytes(workspace, x)
     elif dw is not None:
         size = _workspace_size(*params, packed=cu_seqlens is not None)
         workspace = x.new_empty(size, dtype=torch.uint8)
@@ -1210,7 +1218,7 @@ def join_norm_backward(x_out, h, w_before, dy, dx_out=None, *, w_after=None, cha
     if dy is not None or h is not None:
         size = 0
         if workspace is not None:
-            size = workspace.numel() * workspace.element_size()
+            size = _workspace_bytes(workspace, x_out)
         elif dy is not None or dw_after is not None or dchannel is not None:
             size = _workspace_size(*params, packed=cu_seqlens is not None)
             workspace = x_out.new_empty(size, dtype=torch.uint8)

@@ -123,20 +123,23 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_backward_kernel(GateAr
     load_weights(a, p, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[i] = 0.f;
+    Raw8<BF16> xr{}, gr{}, yr{};
+    auto fetch = [&](int64_t n) {
+        if (!p.live || n >= p.end) return;
+        const size_t oy = offset_y(a, p, n);
+        fetch8(a.x, offset_x(a, p, n), xr);
+        fetch8(a.dy, oy, yr);
+        if (GATE != kNone) fetch8(a.g, oy, gr);
+    };
+    fetch(p.n);
     const int64_t wave_first = __builtin_amdgcn_readfirstlane((int)p.n);
     for (int64_t m = wave_first, n = p.n; m < p.end; m += p.step, n += p.step) {
         float x[8], g[8], dy[8], dn[8];
-        const bool row = p.live && n < p.end;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = g[i] = dy[i] = 0.f;
-        size_t ox = 0, oy = 0;
-        if (row) {
-            ox = offset_x(a, p, n);
-            oy = offset_y(a, p, n);
-            load8<BF16>(a.x, ox, x);
-            load8<BF16>(a.dy, oy, dy);
-            if (GATE != kNone) load8<BF16>(a.g, oy, g);
-        }
+        const bool row = p.live && n < p.end;  // where not, the lane holds some other row: nothing of it is stored or summed
+        unpack8(xr, x);
+        unpack8(yr, dy);
+        unpack8(gr, g);
+        fetch(n + p.step);  // the next row's loads are under way while this one is worked on
         float s = 0.f, c = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -161,8 +164,8 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_backward_kernel(GateAr
             x[i] = r * (dn[i] * w[i] - n_ * mean);
         }
         if (row) {
-            store8<BF16>(a.dx, ox, x);
-            if (GATE != kNone) store8<BF16>(a.dg, oy, g);
+            store8<BF16>(a.dx, offset_x(a, p, n), x);
+            if (GATE != kNone) store8<BF16>(a.dg, offset_y(a, p, n), g);
         }
     }
     if (!a.part) return;

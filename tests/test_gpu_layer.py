@@ -176,6 +176,51 @@ def test_captured_chain_replays_identically():
         assert all(torch.equal(a, b) for a, b in zip(kept, want)), f"replay {rep}"
 
 
+@pytest.mark.parametrize("D", [8192, 16384])
+def test_captured_wide_rows(D):
+    """Rows wide enough that the gradients' kernel asks for more LDS than a launch gets by itself."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    r = lambda *s: torch.randn(*s, device="cuda").bfloat16()
+    xo, h, dy, dxo = (r(70, D) for _ in range(4))
+    w = [1 + 0.1 * torch.randn(D, device="cuda") for _ in range(3)]
+    run = lambda: sla.join_norm_backward(xo, h, w[0], dy, dxo, w_after=w[1], channel_scale=w[2])
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        kept = run()
+    for rep in range(3):
+        for t in (xo, h, dy, dxo):
+            t.copy_(r(70, D))
+        want = run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(kept[n], want[n]) for n in want), f"replay {rep}"
+
+
+def test_host_tensors_workspaces_and_outputs_are_checked():
+    """What only a machine with a GPU can be asked: tensors of two devices, a workspace that is too small or elsewhere, an output on
+    an input that is laid out differently."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    x = torch.ones(2, 4, 4, 64, device="cuda")
+    w, f = torch.ones(64, device="cuda"), torch.ones(32, dtype=torch.float64)
+    for call in (lambda: sla.rotary(x, x, f), lambda: sla.norm_gate(x, x.cpu(), w), lambda: sla.norm_gate(x, x, w.cpu()),
+                 lambda: sla.norm_gate(x, x, w, head_major=True, out=x), lambda: sla.join_norm(x, x.cpu(), w),
+                 lambda: sla.norm_gate_backward(x, x, w, x, workspace=torch.empty(1 << 20, dtype=torch.uint8)),
+                 lambda: sla.rotary(x, x, f.cuda(), q_out=x), lambda: sla.rotary(x, x.clone(), f.cuda(), q_out=x, k_out=x)):
+        with pytest.raises(ValueError):
+            call()
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    for call in (lambda: sla.norm_gate_backward(x, x, w, x, workspace=small), lambda: sla.join_norm_backward(x, x, w, x, workspace=small)):
+        with pytest.raises(sla.SlaError) as e:
+            call()
+        assert e.value.status == -6
+
+
 def test_two_streams_at_once():
     """Calls on a stream of their own run there: after work that is queued on it, beside calls on another stream."""
     import torch

@@ -269,6 +269,8 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
         lambda: sla.rotary(q[0], q[0], f, head_major=True),
         lambda: sla.rotary(q, None, f, k_out=q),
         lambda: sla.rotary(q, q, f, q_out=q.bfloat16()),
+        lambda: sla.rotary(q, q.clone(), f, q_out=q, k_out=q),
+        lambda: sla.rotary(q, q, f, q_out=q),
         lambda: sla.norm_gate(q, q, w),
         lambda: sla.norm_gate(q, None, w),
         lambda: sla.norm_gate(q, q, w, gate="none"),
@@ -280,6 +282,7 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
         lambda: sla.norm_gate(q, q.bfloat16(), w),
         lambda: sla.norm_gate(q, q, w, cu_seqlens=i32(3)),
         lambda: sla.norm_gate(q, q, w, head_major=True, out=q),            # the output is [B,T,H,dv]
+        lambda: sla.norm_gate(torch.zeros(1, 4, 4, 64), torch.zeros(1, 4, 4, 64), w, head_major=True, out=torch.zeros(1, 4, 4, 64)),
         lambda: sla.norm_gate_backward(q, q, w, q[:, :4]),
         lambda: sla.join_norm(D, D, w),
         lambda: sla.join_norm(D, D[:, :4], w),
