@@ -59,26 +59,34 @@ __device__ __forceinline__ void row_sums(float (&s)[N], int row_waves, float* re
     }
 }
 
+// A row of a tensor, the same in a whole wave.  It is held in scalar registers: a lane's address is then 32 bits beside it, where
+// the compiler would else keep one of 64 for each tensor and piece across the walk over rows.
+template <bool BF16, typename P>
+__device__ __forceinline__ P* row_of(P* x, int64_t n, int D) {
+    uint64_t at = (uint64_t)x + (size_t)n * D * (BF16 ? 2 : 4);
+    asm("" : "+s"(at));
+    return (P*)(__attribute__((address_space(1))) P*)at;
+}
+
 template <bool XBF, bool HBF, int V>
 __global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
     __shared__ float red[2 * 16 * 4];
     int flip = 0;
-    const int wv = threadIdx.x >> 6, slot = wv / a.row_waves;
-    const int col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slot = wv / a.row_waves;
+    const uint32_t col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8, D = a.D;
     int64_t first, end;
     token_range(a.cu, a.B, a.tokens, first, end);
     for (int64_t r0 = first + (int64_t)blockIdx.x * a.rows; r0 < end; r0 += (int64_t)gridDim.x * a.rows) {
         const int64_t n = r0 + slot;
-        const size_t row = (size_t)n * a.D;
         float x[V][8], h[V][8];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[v][i] = h[v][i] = 0.f;
-            const int j = col + v * next;
-            if (j < a.D && n < end) {
-                load8<XBF>(a.x, row + j, x[v]);
-                if (a.h) load8<HBF>(a.h, row + j, h[v]);
+            const uint32_t j = col + v * next;
+            if (j < D && n < end) {
+                load8<XBF>(row_of<XBF>(a.x, n, a.D), j, x[v]);
+                if (a.h) load8<HBF>(row_of<HBF>(a.h, n, a.D), j, h[v]);
             }
         }
         if (a.h) {
@@ -94,8 +102,8 @@ __global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int j = col + v * next;
-                if (j >= a.D) continue;
+                const uint32_t j = col + v * next;
+                if (j >= D) continue;
                 float w[8], c[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = c[i] = 1.f;
@@ -103,7 +111,7 @@ __global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
                 if (a.channel) load8<false>(a.channel, j, c);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] += h[v][i] * rh * w[i] * c[i];
-                if (n < end) store8<XBF>(a.xo, row + j, x[v]);
+                if (n < end) store8<XBF>(row_of<XBF>(a.xo, n, a.D), j, x[v]);
             }
         }
         if (a.y) {
@@ -116,13 +124,13 @@ __global__ __launch_bounds__(1024) void sla_join_norm_kernel(JoinArgs a) {
             const float r = inverse_root(s[0] * a.inv_d + a.eps);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int j = col + v * next;
-                if (j >= a.D || n >= end) continue;
+                const uint32_t j = col + v * next;
+                if (j >= D || n >= end) continue;
                 float w[8];
                 load8<false>(a.w_before, j, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[v][i] *= r * w[i];
-                store8<HBF>(a.y, row + j, x[v]);
+                store8<HBF>(row_of<HBF>(a.y, n, a.D), j, x[v]);
             }
         }
     }
@@ -148,8 +156,8 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
     constexpr bool kAhead = THREADS == 512;
     float* lds = red + 2 * 16 * 4;
     int flip = 0;
-    const int wv = threadIdx.x >> 6, slot = wv / a.row_waves;
-    const int col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slot = wv / a.row_waves;
+    const uint32_t col = ((wv - slot * a.row_waves) * 64 + (threadIdx.x & 63)) * 8, next = a.row_waves * 64 * 8, D = a.D;
     const bool reads_h = a.w_after || a.channel;
     const int planes = reads_h ? 2 : 1, width = next * V;
     Raw8<XBF> x_[V], dxo_[V];
@@ -157,40 +165,39 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
     float wb[8], cw[8], pw[8], pp[8];
     // w_before (0 without dy), and scale * channel * w_after, at piece v; past the row's end nothing is read
     auto before = [&](int v, float (&w)[8]) {
-        const int j = col + v * next;
+        const uint32_t j = col + v * next;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = 0.f;
-        if (a.dy && j < a.D) load8<false>(a.w_before, j, w);
+        if (a.dy && j < D) load8<false>(row_of<false>(a.w_before, 0, 0), j, w);
     };
     auto after = [&](int v, float (&w)[8]) {
-        const int j = col + v * next;
+        const uint32_t j = col + v * next;
         float u[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = a.scale;
-        if (j >= a.D) return;
+        if (j >= D) return;
         if (a.w_after) {
-            load8<false>(a.w_after, j, u);
+            load8<false>(row_of<false>(a.w_after, 0, 0), j, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] *= u[i];
         }
         if (a.channel) {
-            load8<false>(a.channel, j, u);
+            load8<false>(row_of<false>(a.channel, 0, 0), j, u);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] *= u[i];
         }
     };
     auto fetch = [&](int64_t n) {
-        const size_t row = (size_t)n * a.D;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int j = col + v * next;
-            if (j >= a.D) continue;
+            const uint32_t j = col + v * next;
+            if (j >= D) continue;
             if (a.dy) {
-                fetch8(a.x, row + j, x_[v]);
-                fetch8(a.dy, row + j, dy_[v]);
+                fetch8(row_of<XBF>(a.x, n, a.D), j, x_[v]);
+                fetch8(row_of<HBF>(a.dy, n, a.D), j, dy_[v]);
             }
-            if (a.dxo) fetch8(a.dxo, row + j, dxo_[v]);
-            if (reads_h) fetch8(a.h, row + j, h_[v]);
+            if (a.dxo) fetch8(row_of<XBF>(a.dxo, n, a.D), j, dxo_[v]);
+            if (reads_h) fetch8(row_of<HBF>(a.h, n, a.D), j, h_[v]);
         }
     };
 #pragma unroll
@@ -214,7 +221,6 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
     if (kAhead && r0 + slot < end) fetch(r0 + slot);
     for (; r0 < end; r0 += step) {
         const int64_t n = r0 + slot;
-        const size_t row = (size_t)n * a.D;
         const bool there = n < end;  // where not, the lanes hold some other row: nothing of it is stored or summed
         if (!kAhead && there) fetch(n);
         float dx[V][8], h[V][8];
@@ -245,7 +251,7 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
             const float r = inverse_root(s[0] * a.inv_d + a.eps), mean = s[1] * r * a.inv_d;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int j = col + v * next;
+                const uint32_t j = col + v * next;
                 float x[8], dy[8];
                 if (V > 1) before(v, wb);
                 unpack8(xr[v], x);
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
                     dx[v][i] += r * (dy[i] * wb[i] - n_ * mean);
                 }
                 if (V > 1 && a.part) add_to(lds + j, pw);
-                if (j < a.D && there) store8<XBF>(a.dx, row + j, dx[v]);
+                if (j < D && there) store8<XBF>(row_of<XBF>(a.dx, n, a.D), j, dx[v]);
             }
         }
         if (!a.dh) continue;
@@ -278,10 +284,10 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
         const float mean = a.w_after ? t[0] * a.inv_d : 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int j = col + v * next;
+            const uint32_t j = col + v * next;
 #pragma unroll
             for (int i = 0; i < 8; ++i) dx[v][i] = rh * (dx[v][i] - h[v][i] * mean);
-            if (j < a.D && there) store8<HBF>(a.dh, row + j, dx[v]);
+            if (j < D && there) store8<HBF>(row_of<HBF>(a.dh, n, a.D), j, dx[v]);
         }
     }
     if (!a.part) return;
@@ -296,8 +302,8 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
     const int others = V == 1 ? a.rows - 1 : 1;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int j = col + v * next;
-        if (j >= a.D) continue;
+        const uint32_t j = col + v * next;
+        if (j >= D) continue;
         float u[8];
         if (V > 1) {
 #pragma unroll
