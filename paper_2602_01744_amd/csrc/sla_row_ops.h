@@ -32,13 +32,10 @@ __device__ __forceinline__ void fetch8(const void* x, size_t off, Raw8<false>& r
     r.a = *(const f4*)((const float*)x + off);
     r.b = *(const f4*)((const float*)x + off + 4);
 }
-// The same where only the elements themselves are aligned (the hardware takes such addresses).
-typedef u4 u4_at2 __attribute__((aligned(2)));
-typedef f4 f4_at4 __attribute__((aligned(4)));
-__device__ __forceinline__ void fetch8_anywhere(const void* x, size_t off, Raw8<true>& r) { r.v = *(const u4_at2*)((const uint16_t*)x + off); }
-__device__ __forceinline__ void fetch8_anywhere(const void* x, size_t off, Raw8<false>& r) {
-    r.a = *(const f4_at4*)((const float*)x + off);
-    r.b = *(const f4_at4*)((const float*)x + off + 4);
+__device__ __forceinline__ void put8(void* x, size_t off, const Raw8<true>& r) { *(u4*)((uint16_t*)x + off) = r.v; }
+__device__ __forceinline__ void put8(void* x, size_t off, const Raw8<false>& r) {
+    *(f4*)((float*)x + off) = r.a;
+    *(f4*)((float*)x + off + 4) = r.b;
 }
 __device__ __forceinline__ void unpack8(const Raw8<true>& r, float (&f)[8]) {
 #pragma unroll
@@ -72,19 +69,6 @@ __device__ __forceinline__ void store8(void* y, size_t off, const float (&f)[8])
     } else {
         *(f4*)((float*)y + off) = f4{f[0], f[1], f[2], f[3]};
         *(f4*)((float*)y + off + 4) = f4{f[4], f[5], f[6], f[7]};
-    }
-}
-
-template <bool BF16>
-__device__ __forceinline__ void store8_anywhere(void* y, size_t off, const float (&f)[8]) {
-    if constexpr (BF16) {
-        u4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = lane_ops::pack2(f[2 * i], f[2 * i + 1]);
-        *(u4_at2*)((uint16_t*)y + off) = v;
-    } else {
-        *(f4_at4*)((float*)y + off) = f4{f[0], f[1], f[2], f[3]};
-        *(f4_at4*)((float*)y + off + 4) = f4{f[4], f[5], f[6], f[7]};
     }
 }
 
