@@ -425,7 +425,8 @@ size_t sla_gate_logits_backward_workspace_bytes(const sla_params* p);
  *   frequencies      [rotary/2]  fp64    radians a token, one for each pair
  *   positions        NULL: a sequence's tokens have positions 0, 1, ...;  else int32 [B]: the position of every sequence's first
  *                    token;  with SLA_FLAG_TOKEN_POSITIONS int32 [B,T] (packed [T]): the position of every token
- * q_out may be q and k_out k (the same address); nothing else may overlap.  sla_rotary_backward turns the cotangents of
+ * q_out may be q and k_out k (the same address); nothing else may overlap.  For a fixed table the result of a token does not
+ * depend on the batch it is in.  sla_rotary_backward turns the cotangents of
  * the outputs back (and scales them by m): dq_out, dk_out take the place of q, k and dq, dk that of q_out, k_out.
  */
 #define SLA_FLAG_ADJACENT_PAIRS 2

@@ -6,11 +6,14 @@
 //     m = h r_h, P = sum scale dX m,  dm = scale dX c w_after                  dw_after = c P,  dc = w_after P
 //     dh = r_h (dm - m mean(dm m))         or, without the norm behind the block, dh = scale dX c,  dc = sum scale dX h.
 //
-// Streaming passes over 4 (backward up to 6) tensors.  A row of the stream lies in the registers of one to sixteen waves, 8 V
-// elements a lane, from its first read to its last write, so nothing is read twice; a sum over it is a few lane exchanges
-// and, where waves share the row, one exchange through LDS.  x' goes into y before it is rounded to the stream's type.  The
-// backward's workgroups walk over rows with the sums for w_before and P in registers and leave one partial sum each; a
-// second kernel adds these in a fixed order: no atomics, so results do not change from run to run.
+// Streaming passes over 4 (backward up to 6) tensors, bound by memory.  A row of the stream lies in the registers of one to
+// sixteen waves, eight elements a lane (sixteen in rows over 8192), from its first read to its last write, so nothing is read
+// twice; a sum over it is a few lane exchanges and, where waves share the row, one exchange through LDS.  x' goes into y before
+// it is rounded to the stream's type.  The backward's workgroups walk over rows with the sums for w_before and P in registers
+// and leave one partial sum each; a second kernel adds these in a fixed order: no atomics, so results do not change from run
+// to run.  Measured (a large copy reaches 5.4 TB/s, more where the last-level cache holds part of it): bf16, 32768 rows of 1024
+// with both norms, 268 MB, 48 us; gradients of 16384 rows of 2048, fp32 stream, both norms and a scale, 604 MB, 120 us.  Rows
+// over 8192 stay at half of that rate: one workgroup fills a compute unit, so its loads and its arithmetic take turns.
 #include "sla_row_ops.h"
 
 namespace sla {
@@ -152,7 +155,7 @@ __device__ __forceinline__ void add_to(float* at, float (&f)[8]) {
 // Up to 8192 (THREADS 1024) the registers hold the weights, beyond that (V = 2) neither: the sums over tokens move to LDS too.
 template <bool XBF, bool HBF, int V, int THREADS>
 __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArgs a) {
-    extern __shared__ float red[];  // the exchange buffer; after it [V == 1 ? rows - 1 : 1][planes][row_waves * 64 * 8 * V] sums
+    extern __shared__ __align__(16) float red[];  // the exchange buffer; after it [V == 1 ? rows - 1 : 1][planes][row_waves * 64 * 8 * V] sums
     constexpr bool kAhead = THREADS == 512;
     float* lds = red + 2 * 16 * 4;
     int flip = 0;
@@ -367,7 +370,9 @@ int check_join(const sla_join_norm_params* p, const int32_t* cu) {
 
 int64_t tokens_of(const sla_join_norm_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
 
-// How a row lies over lanes: one piece of eight a lane and as many waves as that takes, or two pieces in rows over 8192.  More rows share a workgroup of `waves` waves where theirs leave room.
+// How a row lies over lanes: one piece of eight a lane and as many waves as that takes (bf16, 16384 rows of 2048 with one, two
+// and four pieces 45.5, 47.7, 51.8 us; fp32 stream 78, 81, 92 us), or two pieces in rows over 8192.  More rows share a
+// workgroup of `waves` waves where theirs leave room.
 struct Split {
     int v, row_waves, rows, threads;
 };

@@ -4,7 +4,9 @@
 // and its gradients for the cotangent dy of y, from x and g again (nothing is kept from the forward call),
 //     dn = dy w act(g),  dx = r (dn - n mean(dn n)),  dg = dy n w act'(g),  dw = sum over tokens of dy n act(g).
 //
-// Streaming passes over 3 (backward 5) tensors, a few tens of flops an element.  A head's vector lies in dv/8 lanes (a power of
+// Streaming passes over 3 (backward 5) tensors, a few tens of flops an element, bound by memory.  Measured in bf16 (a large copy
+// reaches 5.4 TB/s, more where the last-level cache holds part of it): T=65536 16 heads of 128, 805 MB, 142 us; gradients B=8
+// T=4096 16 heads of 128, 671 MB, 131 to 136 us.  A head's vector lies in dv/8 lanes (a power of
 // two of them is set aside), eight elements each, so its sums are a few lane exchanges and nothing is read twice.  A wave
 // covers as many heads of a token as divide H, then several tokens: a lane keeps to one head, whose weights stay in
 // registers.  dw is summed in two stages in a fixed order: over a workgroup's tokens in registers and LDS, then over the

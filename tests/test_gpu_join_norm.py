@@ -82,7 +82,9 @@ def _both(x, h, wb, wa, c, dy, dxo, scale, types, **kw):
 
 @pytest.mark.parametrize("types", list(TYPES))
 @pytest.mark.parametrize("lead,D", [((1, 1), 1024), ((2, 37), 1024), ((3, 5), 2048), ((7,), 8), ((130,), 264), ((2, 3), 4104), ((5,), 8192),
-                                    ((3,), 16384), ((2, 701), 520), ((4,), 1536)])
+                                    ((3,), 16384), ((2, 701), 520), ((4,), 1536),
+                                    # more rows than the gradients' workgroups take at a time
+                                    ((9001,), 64), ((1100,), 4096), ((300,), 8192), ((300,), 8200)])
 @pytest.mark.parametrize("after,channel", [(0, 0), (1, 1)])
 def test_parity(types, lead, D, after, channel):
     x, h, wb, wa, c, dy, dxo = _inputs(D + lead[0], lead, D, types, after, channel)

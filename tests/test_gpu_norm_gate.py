@@ -50,7 +50,8 @@ def _check_backward(got, x, g, w, dy, gate, dtype, eps=EPS):
 
 SHAPES = [  # lead, H, dv
     ((2, 37), 4, 128), ((1, 1), 1, 64), ((64, 1), 16, 128), ((1, 203), 5, 64), ((3, 11), 12, 256), ((1, 130), 3, 8), ((2, 5), 7, 40),
-    ((1, 19), 2, 512), ((1, 9), 1, 504), ((1, 700), 64, 16), ((2, 3), 1, 96)]
+    ((1, 19), 2, 512), ((1, 9), 1, 504), ((1, 700), 64, 16), ((2, 3), 1, 96),
+    ((1, 2500), 64, 16), ((1, 2300), 4, 256)]  # more tokens than the gradients' workgroups take at a time
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -68,7 +69,7 @@ def test_parity(dtype, lead, H, dv, gate, weight):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("B,T,H,dv", [(2, 33, 4, 128), (3, 17, 5, 64), (1, 70, 1, 256), (4, 1, 6, 40)])
+@pytest.mark.parametrize("B,T,H,dv", [(2, 33, 4, 128), (3, 17, 5, 64), (1, 70, 1, 256), (4, 1, 6, 40), (2, 2600, 16, 64)])
 @pytest.mark.parametrize("weight", ["shared", "heads"])
 def test_head_major(dtype, B, T, H, dv, weight):
     """x as sla_forward leaves it in its head-major layout, everything else token-major: bits as from the other layout."""

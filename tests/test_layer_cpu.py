@@ -307,6 +307,39 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
             pytest.fail(f"call {i} was not refused")
 
 
+def test_calls_run_on_their_tensors_device(monkeypatch):
+    """Tensors of another GPU than the current one: the call is made with theirs current, on their current stream."""
+    import contextlib
+
+    import torch
+    from paper_2602_01744_amd import binding
+
+    current = [0]
+
+    @contextlib.contextmanager
+    def device(d):
+        before, current[0] = current[0], int(d)
+        yield
+        current[0] = before
+
+    class Tensor:
+        def __init__(self, d):
+            self.d, self.device = d, f"cuda:{d}"
+
+        def get_device(self):
+            return self.d
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 1000 + d, raising=False)
+    seen = []
+    for d in (0, 1):
+        binding._run(lambda *a: seen.append((current[0],) + a) or 0, Tensor(d), 7)
+    assert seen == [(0, 7, 1000), (1, 7, 1001)] and current == [0]
+    with pytest.raises(ValueError):
+        binding._run(lambda *a: pytest.fail("called"), Tensor(-1), 7)
+
+
 def test_host_code_under_sanitizers(tmp_path):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     if not (os.path.exists(hipcc) or shutil.which(hipcc)):
