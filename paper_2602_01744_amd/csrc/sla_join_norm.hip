@@ -10,10 +10,10 @@
 // sixteen waves, eight elements a lane (sixteen in rows over 8192), from its first read to its last write, so nothing is read
 // twice; a sum over it is a few lane exchanges and, where waves share the row, one exchange through LDS.  x' goes into y before
 // it is rounded to the stream's type.  The backward's workgroups walk over rows with the sums for w_before and P in registers
-// and leave one partial sum each; a second kernel adds these in a fixed order: no atomics, so results do not change from run
-// to run.  Measured (a large copy reaches 5.4 TB/s, more where the last-level cache holds part of it): bf16, 32768 rows of 1024
-// with both norms, 268 MB, 48 us; gradients of 16384 rows of 2048, fp32 stream, both norms and a scale, 604 MB, 120 us.  Rows
-// over 8192 stay at half of that rate: one workgroup fills a compute unit, so its loads and its arithmetic take turns.
+// and leave one partial sum each; a second kernel adds these, in 64 bits and a fixed order: no atomics, so results do not change
+// from run to run.  Measured (a large copy reaches 5.4 TB/s, more where the last-level cache holds part of it): bf16, 32768 rows
+// of 1024 with both norms, 268 MB, 48 us; gradients of 16384 rows of 2048, fp32 stream, both norms and a scale, 604 MB, 120 us.
+// Rows over 8192 stay at half of that rate: one workgroup fills a compute unit, so its loads and its arithmetic take turns.
 #include "sla_row_ops.h"
 
 namespace sla {
@@ -329,32 +329,33 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
     }
 }
 
-// A workgroup sums 16 adjacent columns of a plane: 64 threads a column, four of them in a wave.
+// A workgroup sums 16 adjacent columns of a plane in 64 bits: 64 threads a column, four of them in a wave.
 constexpr int kSumColumns = 16, kSumRows = 64;
 __global__ __launch_bounds__(kSumColumns * kSumRows) void sla_column_sums_kernel(const float* part, int nparts, int planes, int width,
                                                                                float* out0, float* out1, const float* by1,
                                                                                float* out2, const float* by2) {
-    __shared__ float red[kSumRows / 4][kSumColumns];
+    __shared__ double red[kSumRows / 4][kSumColumns];
     const int c = threadIdx.x % kSumColumns, rr = threadIdx.x / kSumColumns, wv = threadIdx.x >> 6;
     const int per_plane = (width + kSumColumns - 1) / kSumColumns;
     const int plane = blockIdx.x / per_plane, j = (blockIdx.x - plane * per_plane) * kSumColumns + c;
-    float s = 0.f;
+    double s = 0.0;
     if (j < width) {
 #pragma unroll 8
         for (int n = rr; n < nparts; n += kSumRows) s += part[((size_t)n * planes + plane) * width + j];
     }
-    s = lane_ops::all_groups(s);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
     if (threadIdx.x % 64 < kSumColumns) red[wv][c] = s;
     __syncthreads();
     if (rr > 0 || j >= width) return;
-    s = 0.f;
+    s = 0.0;
 #pragma unroll
     for (int w = 0; w < kSumRows / 4; ++w) s += red[w][c];
     if (plane == 0) {
-        if (out0) out0[j] = s;
+        if (out0) out0[j] = (float)s;
     } else {
-        if (out1) out1[j] = by1 ? s * by1[j] : s;
-        if (out2) out2[j] = by2 ? s * by2[j] : s;
+        if (out1) out1[j] = (float)(by1 ? s * by1[j] : s);
+        if (out2) out2[j] = (float)(by2 ? s * by2[j] : s);
     }
 }
 

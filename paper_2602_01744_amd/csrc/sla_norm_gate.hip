@@ -9,8 +9,8 @@
 // T=4096 16 heads of 128, 671 MB, 131 to 136 us.  A head's vector lies in dv/8 lanes (a power of
 // two of them is set aside), eight elements each, so its sums are a few lane exchanges and nothing is read twice.  A wave
 // covers as many heads of a token as divide H, then several tokens: a lane keeps to one head, whose weights stay in
-// registers.  dw is summed in two stages in a fixed order: over a workgroup's tokens in registers and LDS, then over the
-// workgroups' partial sums; no atomics, so results do not change from run to run.
+// registers.  dw is summed in two stages in a fixed order: over a workgroup's tokens in registers and LDS, then, in 64 bits, over
+// the workgroups' partial sums; no atomics, so results do not change from run to run.
 #include "sla_row_ops.h"
 
 namespace sla {
