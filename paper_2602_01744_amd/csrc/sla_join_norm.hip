@@ -13,7 +13,7 @@
 // and leave one partial sum each; a second kernel adds these, in 64 bits and a fixed order: no atomics, so results do not change
 // from run to run.  Measured (a large copy reaches 5.4 TB/s, more where the last-level cache holds part of it): bf16, 32768 rows
 // of 1024 with both norms, 268 MB, 48 us; gradients of 16384 rows of 2048, fp32 stream, both norms and a scale, 604 MB, 120 us.
-// Rows over 8192 stay at half of that rate: one workgroup fills a compute unit, so its loads and its arithmetic take turns.
+// Rows over 8192 stay at half of that rate: one workgroup fills a compute unit without room to load ahead.
 #include "sla_row_ops.h"
 
 namespace sla {
@@ -151,12 +151,11 @@ __device__ __forceinline__ void add_to(float* at, float (&f)[8]) {
     store8<false>(at, 0, u);
 }
 
-// Rows up to 4096 (THREADS 512): the weights stay in registers, and the next row's loads are under way while a row is worked on.
-// Up to 8192 (THREADS 1024) the registers hold the weights, beyond that (V = 2) neither: the sums over tokens move to LDS too.
-template <bool XBF, bool HBF, int V, int THREADS>
-__global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArgs a) {
+// Rows up to 8192 (V = 1): the weights stay in registers, and the next row's loads are under way while a row is worked on (4096
+// rows of 8192, fp32 stream: 95 -> 88 us).  Wider ones (V = 2) have registers for neither, and their sums over tokens move to LDS.
+template <bool XBF, bool HBF, int V>
+__global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a) {
     extern __shared__ __align__(16) float red[];  // the exchange buffer; after it [V == 1 ? rows - 1 : 1][planes][row_waves * 64 * 8 * V] sums
-    constexpr bool kAhead = THREADS == 512;
     float* lds = red + 2 * 16 * 4;
     int flip = 0;
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), slot = wv / a.row_waves;
@@ -221,11 +220,11 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
     token_range(a.cu, a.B, a.tokens, first, end);
     const int64_t step = (int64_t)gridDim.x * a.rows;
     int64_t r0 = first + (int64_t)blockIdx.x * a.rows;
-    if (kAhead && r0 + slot < end) fetch(r0 + slot);
+    if (V == 1 && r0 + slot < end) fetch(r0 + slot);
     for (; r0 < end; r0 += step) {
         const int64_t n = r0 + slot;
         const bool there = n < end;  // where not, the lanes hold some other row: nothing of it is stored or summed
-        if (!kAhead && there) fetch(n);
+        if (V > 1 && there) fetch(n);
         float dx[V][8], h[V][8];
         float s[3] = {0.f, 0.f, 0.f};
         Raw8<XBF> xr[V];
@@ -247,7 +246,7 @@ __global__ __launch_bounds__(THREADS) void sla_join_norm_backward_kernel(JoinArg
                 s[2] += h[v][i] * h[v][i];
             }
         }
-        if (kAhead && n + step < end) fetch(n + step);
+        if (V == 1 && n + step < end) fetch(n + step);
         row_sums(s, a.row_waves, red, flip);
         const float rh = a.w_after ? inverse_root(s[2] * a.inv_d + a.eps) : 1.f;
         if (a.dy) {
@@ -486,14 +485,14 @@ int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, con
     a.row_waves = s.row_waves; a.rows = s.rows;
     const unsigned blocks = backward_workgroups(s, a.tokens);
     const size_t lds = (2 * 16 * 4 + (size_t)(s.v == 1 ? s.rows - 1 : 1) * planes * s.row_waves * 64 * 8 * s.v) * sizeof(float);
-#define SLA_JN(X, Y, V, N)                                                                                              \
+#define SLA_JN(X, Y, V)                                                                                                 \
     do {                                                                                                                \
-        const auto kernel = sla_join_norm_backward_kernel<X, Y, V, N>;                                                    \
+        const auto kernel = sla_join_norm_backward_kernel<X, Y, V>;                                                       \
         if (!allow_lds(kernel, lds)) return SLA_ERR_HIP;                                                                 \
         hipLaunchKernelGGL(kernel, dim3(blocks), dim3(s.threads), lds, (hipStream_t)stream, a);                          \
     } while (0)
 #define SLA_JN_V(X, Y) \
-    if (s.v == 2) SLA_JN(X, Y, 2, 1024); else if (s.threads == 1024) SLA_JN(X, Y, 1, 1024); else SLA_JN(X, Y, 1, 512)
+    if (s.v == 1) SLA_JN(X, Y, 1); else SLA_JN(X, Y, 2)
     if (p->dtype == SLA_F32) { SLA_JN_V(false, false); }
     else if (p->x_dtype == SLA_F32) { SLA_JN_V(false, true); }
     else { SLA_JN_V(true, true); }
