@@ -457,7 +457,8 @@ int sla_rotary_backward(const sla_rotary_params* p, const void* dq_out, const vo
  *            that share it) in a fixed order; zeros for an empty batch
  *   workspace  sla_norm_gate_backward_workspace_bytes(p, packed) bytes, 16-byte aligned, for dw (packed: with cu_seqlens);
  *            contents undefined before and after, calls that share it must not overlap
- * y may be g or, without SLA_FLAG_HEAD_MAJOR, x (the same address); nothing else may overlap.
+ * y may be g or, without SLA_FLAG_HEAD_MAJOR, x (the same address); nothing else may overlap.  Sums of squares are fp32: a
+ * vector with a value over 1e19 is divided by infinity.
  */
 typedef enum { SLA_GATE_NONE = 0, SLA_GATE_SILU = 1, SLA_GATE_SIGMOID = 2 } sla_gate;
 #define SLA_FLAG_HEAD_WEIGHTS 2

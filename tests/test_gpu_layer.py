@@ -221,6 +221,63 @@ def test_host_tensors_workspaces_and_outputs_are_checked():
         assert e.value.status == -6
 
 
+def test_offsets_past_32_bits():
+    """Tensors of more than 2^32 bytes: their last rows come out as those of small ones, in the outputs and the gradients."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    if torch.cuda.mem_get_info()[0] < 40 * 2 ** 30:
+        pytest.skip("not enough memory")
+    r = lambda *s: torch.randn(*s, device="cuda").bfloat16()
+    w = 1 + 0.1 * torch.randn(16384, device="cuda")
+    rows, tail = 135000, [r(5, 16384) for _ in range(4)]  # 4.4 GB a tensor
+    big = [torch.zeros(rows, 16384, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    for a, b in zip(big, tail):
+        a[-5:] = b
+    got, want = (sla.join_norm(t[0], t[1], w, w_after=w) for t in (big, tail))
+    assert all(torch.equal(a[-5:], b) for a, b in zip(got, want))
+    got, want = (sla.join_norm_backward(t[0], t[1], w, t[2], t[3], w_after=w) for t in (big, tail))
+    assert torch.equal(got["dx"][-5:], want["dx"]) and torch.equal(got["dh"][-5:], want["dh"])
+    assert rel_err(numpy64(got["dw_before"]), numpy64(want["dw_before"])) <= 1e-6  # zero rows add nothing; another order
+    del got, want
+    heads = [t.view(1, -1, 32, 512) for t in big[:3]]
+    small = [t.view(1, -1, 32, 512) for t in tail[:3]]
+    n = small[0].shape[1]
+    v = w[:512].contiguous()
+    assert torch.equal(sla.norm_gate(heads[0], heads[1], v)[:, -n:], sla.norm_gate(small[0], small[1], v))
+    got, want = (sla.norm_gate_backward(t[0], t[1], v, t[2]) for t in (heads, small))
+    assert torch.equal(got["dx"][:, -n:], want["dx"]) and torch.equal(got["dg"][:, -n:], want["dg"])
+
+
+def test_offsets_of_sequences_are_clamped():
+    """No content of cu_seqlens makes a kernel leave the tensors: offsets under 0, past the last token, and out of order."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    T = 12
+    x, g, w = torch.randn(T, 4, 64, device="cuda"), torch.randn(T, 4, 64, device="cuda"), torch.ones(64, device="cuda")
+    f, _ = sla.rotary_frequencies(64)
+    for cu in ([-3, 5, 99], [0, 9, 2, 12], [7, 3], [50, 60], [-9, -2]):
+        lo = min(max(cu[0], 0), T)
+        hi = max(min(max(cu[-1], 0), T), lo)
+        c = torch.tensor(cu, dtype=torch.int32, device="cuda")
+        y = torch.full_like(x, 7.0)
+        sla.norm_gate(x, g, w, cu_seqlens=c, out=y)
+        want = torch.full_like(x, 7.0)
+        if hi > lo:
+            want[lo:hi] = sla.norm_gate(x[lo:hi].contiguous(), g[lo:hi].contiguous(), w)
+        assert torch.equal(y, want), cu
+        q = torch.full_like(x, 7.0)
+        sla.rotary(x, None, f, cu_seqlens=c, start=torch.zeros(len(cu) - 1, dtype=torch.int32, device="cuda"), q_out=q)
+        assert bool((q[:lo] == 7.0).all()) and bool((q[hi:] == 7.0).all()) and bool(torch.isfinite(q).all())
+        v, ones = x.view(T, 256), torch.ones(256, device="cuda")
+        a, b = torch.full_like(v, 7.0), torch.full_like(v, 7.0)
+        sla.join_norm(v, g.view(T, 256), ones, cu_seqlens=c, x_out=a, y=b)
+        sla.join_norm_backward(v, g.view(T, 256), ones, v, v, cu_seqlens=c)
+        assert bool((a[:lo] == 7.0).all()) and bool((b[hi:] == 7.0).all())
+        assert hi == lo or torch.equal(a[lo:hi], (v + g.view(T, 256))[lo:hi])
+
+
 def test_two_streams_at_once():
     """Calls on a stream of their own run there: after work that is queued on it, beside calls on another stream."""
     import torch
