@@ -246,9 +246,10 @@ int sla_norm_gate(const sla_norm_gate_params* p, const void* x, const void* g, c
     GateArgs a{};
     layout(*p, a);
     a.x = x; a.g = g; a.w = w; a.y = y; a.cu = cu_seqlens;
-    // Rows that lie apart in x want fewer workgroups that walk on: bf16, B=8 T=2048 16 heads of 128, head-major 37.2 us with 8 a
-    // compute unit, 43.6 with 64; T=65536 token-major 151 and 142 us.
-    const dim3 grid(workgroups(a, tokens_of(*p, cu_seqlens), kComputeUnits * (a.head_major ? 8 : 64)));
+    // Rows that lie apart in x want fewer workgroups that walk on: bf16, B=8 T=2048 16 heads of 128, head-major, with 4, 8, 32 and
+    // 64 a compute unit 36.8, 37.5, 41.9, 43.6 us, B=8 T=4096 4 heads of 256 36.9, 39.6, 44.0 us; token-major, T=65536 16 heads of
+    // 128, 151 us with 8 and 142 with 64.
+    const dim3 grid(workgroups(a, tokens_of(*p, cu_seqlens), kComputeUnits * (a.head_major ? 4 : 64)));
 #define SLA_NG(BF, G) hipLaunchKernelGGL((sla_norm_gate_kernel<BF, G>), grid, dim3(kThreads), 0, (hipStream_t)stream, a)
     if (p->dtype == SLA_BF16) {
         if (p->gate == kNone) SLA_NG(true, kNone); else if (p->gate == kSilu) SLA_NG(true, kSilu); else SLA_NG(true, kSigmoid);
