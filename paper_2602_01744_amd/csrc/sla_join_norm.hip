@@ -174,19 +174,25 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
     };
     auto after = [&](int v, float (&w)[8]) {
         const uint32_t j = col + v * next;
-        float u[8];
+        float u[8], c[8];
+        if constexpr (V == 1) {  // both loads under way at a time
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = a.scale;
-        if (j >= D) return;
-        if (a.w_after) {
-            load8<false>(row_of<false>(a.w_after, 0, 0), j, u);
+            for (int i = 0; i < 8; ++i) u[i] = c[i] = 1.f;
+            if (a.w_after && j < D) load8<false>(row_of<false>(a.w_after, 0, 0), j, u);
+            if (a.channel && j < D) load8<false>(row_of<false>(a.channel, 0, 0), j, c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] *= u[i];
-        }
-        if (a.channel) {
-            load8<false>(row_of<false>(a.channel, 0, 0), j, u);
+            for (int i = 0; i < 8; ++i) w[i] = a.scale * u[i] * c[i];
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] *= u[i];
+            for (int i = 0; i < 8; ++i) w[i] = a.scale;
+            auto times = [&](const float* t) {
+                if (!t || j >= D) return;
+                load8<false>(row_of<false>(t, 0, 0), j, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] *= u[i];
+            };
+            times(a.w_after);
+            times(a.channel);
         }
     };
     auto fetch = [&](int64_t n) {
@@ -203,6 +209,15 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
         }
     };
 #pragma unroll
+    for (int v = 0; v < V; ++v) {
+        x_[v] = {}; dxo_[v] = {}; dy_[v] = {}; h_[v] = {};  // what is never fetched counts as zero
+    }
+    int64_t first, end;
+    token_range(a.cu, a.B, a.tokens, first, end);
+    const int64_t step = (int64_t)gridDim.x * a.rows;
+    int64_t r0 = first + (int64_t)blockIdx.x * a.rows;
+    if (V == 1 && r0 + slot < end) fetch(r0 + slot);  // ahead of the weights, whose way from memory is as long
+#pragma unroll
     for (int i = 0; i < 8; ++i) pw[i] = pp[i] = 0.f;
     if (V == 1) {
         before(0, wb);
@@ -210,17 +225,11 @@ __global__ __launch_bounds__(1024) void sla_join_norm_backward_kernel(JoinArgs a
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        x_[v] = {}; dxo_[v] = {}; dy_[v] = {}; h_[v] = {};  // what is never fetched counts as zero
         if (V > 1 && a.part) {
             store8<false>(lds, col + v * next, pw);
             if (reads_h) store8<false>(lds, width + col + v * next, pp);
         }
     }
-    int64_t first, end;
-    token_range(a.cu, a.B, a.tokens, first, end);
-    const int64_t step = (int64_t)gridDim.x * a.rows;
-    int64_t r0 = first + (int64_t)blockIdx.x * a.rows;
-    if (V == 1 && r0 + slot < end) fetch(r0 + slot);
     for (; r0 < end; r0 += step) {
         const int64_t n = r0 + slot;
         const bool there = n < end;  // where not, the lanes hold some other row: nothing of it is stored or summed
