@@ -1047,6 +1047,7 @@ def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, mag
     elif positions is not None:
         _tensor("positions", positions, device, (T,) if cu_seqlens is not None else (B, T) if q.dim() == 4 else (B,), torch.int32)
         where, flags = positions, flags | FLAG_TOKEN_POSITIONS
+    fresh = q_out is None and k_out is None
     if q_out is None:
         q_out = torch.empty_like(q)
     else:
@@ -1057,8 +1058,9 @@ def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, mag
         k_out = torch.empty_like(k)
     else:
         _tensor("k's output", k_out, device, k.shape, el)
-    if k is not None and (q_out.data_ptr() == k.data_ptr() or k_out.data_ptr() in (q.data_ptr(), q_out.data_ptr())) and q.numel():
-        raise ValueError("an output may lie on its own input only")
+    if not fresh and k is not None and q.numel():
+        _need(q_out.data_ptr() != k.data_ptr() and k_out.data_ptr() not in (q.data_ptr(), q_out.data_ptr()),
+              "an output may lie on its own input only")
     _run(call, q, _params(SlaRotaryParams, _element("q", el), B, T, Hq, Hk, d, 2 * pairs, flags, magnitude), q.data_ptr(),
          _ptr(k), frequencies.data_ptr(), _ptr(where), _ptr(cu_seqlens), q_out.data_ptr(), _ptr(k_out))
     return q_out, k_out
@@ -1090,19 +1092,18 @@ def _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major):
     flags = 0
     if head_major:
         shape, flags = torch.Size((B, T, H, dv)), FLAG_HEAD_MAJOR
-    _need(gate in GATES, f"gate: unknown {gate!r}")
+    kind = GATES.get(gate)
+    if kind is None or (g is None) != (kind == 0):
+        raise ValueError(f"gate: {gate!r} {'with' if g is not None else 'without'} g; expected 'silu' or 'sigmoid' with, 'none' without")
     if g is not None:
-        _need(gate != "none", "gate 'none' takes no g")
         _tensor("g", g, device, shape, el)
-    else:
-        _need(gate == "none", f"gate {gate!r} needs g")
     if w is not None:
         if w.dim() == 2:
             flags |= FLAG_HEAD_WEIGHTS
             _tensor("w", w, device, (H, dv), torch.float32)
         else:
             _tensor("w", w, device, (dv,), torch.float32)
-    return (SlaNormGateParams, _element("x", el), B, T, H, dv, GATES[gate], flags, eps), shape
+    return (SlaNormGateParams, _element("x", el), B, T, H, dv, kind, flags, eps), shape
 
 
 def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None, head_major: bool = False, out=None):
@@ -1185,11 +1186,14 @@ def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float 
               "h: needed, unless only the norm of x is asked for")
     _need(w_before is not None or y is None, "an output y, but no w_before")
     params = _join_args(x, h, y, w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype)
+    if y is not None and x.numel():
+        _need(y.data_ptr() not in (x.data_ptr(), _ptr(x_out)), "y may lie on h only")
     if h is not None:
         if x_out is None:
             x_out = torch.empty_like(x)
         else:
             _tensor("x_out", x_out, x.get_device(), x.shape, x.dtype)
+            _need(x_out.data_ptr() != h.data_ptr() or not x.numel(), "x_out may lie on x only")
     if w_before is not None and y is None:
         y = torch.empty_like(x, dtype=y_dtype) if h is None else torch.empty_like(h)
     _run(load_library().sla_join_norm, x, _params(*params), x.data_ptr(), _ptr(h), _ptr(w_after), _ptr(channel_scale),

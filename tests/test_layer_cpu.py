@@ -295,6 +295,10 @@ def test_binding_refuses_what_the_library_cannot_see(lib):
         lambda: sla.join_norm(D, D, w, cu_seqlens=i32(3)),
         lambda: sla.join_norm(D, D, w, x_out=D.bfloat16()),
         lambda: sla.join_norm(D.transpose(0, 1), D.transpose(0, 1), w),
+        lambda: sla.join_norm(D, D.clone(), w, y=D),
+        lambda: sla.join_norm(D, None, w, y=D),
+        lambda: sla.join_norm(D, w.expand(2, 8, 64).contiguous(), w, x_out=D, y=D),
+        lambda: (lambda h: sla.join_norm(D, h, w, x_out=h))(D.clone()),
         lambda: sla.join_norm_backward(D, D, w, None),
         lambda: sla.join_norm_backward(D, D, None, None),
         lambda: sla.join_norm_backward(D, None, w, D, w_after=w),
