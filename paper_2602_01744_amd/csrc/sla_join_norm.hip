@@ -367,17 +367,21 @@ __global__ __launch_bounds__(kSumColumns * kSumRows) void sla_column_sums_kernel
     }
 }
 
-int check_join(const sla_join_norm_params* p, const int32_t* cu) {
+int64_t tokens_of(const sla_join_norm_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
+
+// The sizes and types of a call or of a query for one.
+int check_sizes(const sla_join_norm_params* p, bool packed) {
     if (!p) return SLA_ERR_NULL;
     if ((p->dtype != SLA_F32 && p->dtype != SLA_BF16) || (p->x_dtype != SLA_F32 && p->x_dtype != SLA_BF16)) return SLA_ERR_UNSUPPORTED;
     if (p->dtype == SLA_F32 && p->x_dtype == SLA_BF16) return SLA_ERR_UNSUPPORTED;  // the stream is never narrower than the blocks
     if (p->B < 0 || p->T < 0 || p->D < 8 || p->D > kMaxWidth || (p->D & 7) || !(p->eps >= 0.f)) return SLA_ERR_SHAPE;
-    if ((cu ? (int64_t)p->T : (int64_t)p->B * p->T) > (int64_t)1 << 30) return SLA_ERR_SHAPE;
-    if (!aligned(cu, 4)) return SLA_ERR_ALIGN;
-    return SLA_OK;
+    return tokens_of(*p, packed) > (int64_t)1 << 30 ? SLA_ERR_SHAPE : SLA_OK;
 }
 
-int64_t tokens_of(const sla_join_norm_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
+int check_join(const sla_join_norm_params* p, const int32_t* cu) {
+    const int rc = check_sizes(p, cu != nullptr);
+    return rc == SLA_OK && !aligned(cu, 4) ? SLA_ERR_ALIGN : rc;
+}
 
 // How a row lies over lanes: one piece of eight a lane and as many waves as that takes (bf16, 16384 rows of 2048 with one, two
 // and four pieces 45.5, 47.7, 51.8 us; fp32 stream 78, 81, 92 us), or two pieces in rows over 8192.  More rows share a
@@ -407,6 +411,9 @@ unsigned backward_workgroups(const Split& s, int64_t tokens) {
     const int64_t n = (tokens + s.rows - 1) / s.rows, most = kComputeUnits * (s.threads == 1024 ? 1 : 2);
     return (unsigned)(n < most ? n : most);
 }
+
+// Bytes of the partial sums that so many workgroups leave (one plane of two may stay unused).
+size_t sums_bytes(unsigned blocks, int D) { return (size_t)blocks * 2 * D * sizeof(float); }
 
 }  // namespace
 
@@ -456,8 +463,8 @@ int sla_join_norm(const sla_join_norm_params* p, const void* x, const void* h, c
 
 size_t sla_join_norm_backward_workspace_bytes(const sla_join_norm_params* p, int packed) {
     using namespace sla;
-    if (check_join(p, nullptr) != SLA_OK || p->B == 0 || p->T == 0) return 0;
-    return (size_t)backward_workgroups(split(p->D, kBackwardWaves), tokens_of(*p, packed)) * 2 * p->D * sizeof(float);
+    if (check_sizes(p, packed != 0) != SLA_OK || p->B == 0 || p->T == 0) return 0;
+    return sums_bytes(backward_workgroups(split(p->D, kBackwardWaves), tokens_of(*p, packed != 0)), p->D);
 }
 
 int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, const void* h, const float* w_after,
@@ -483,16 +490,15 @@ int sla_join_norm_backward(const sla_join_norm_params* p, const void* x_out, con
     if (!work)
         return sums ? launch_column_sums(nullptr, 0, planes, p->D, dw_before, dw_after, nullptr, dchannel_scale, nullptr, (hipStream_t)stream)
                     : SLA_OK;
-    if (sums && (!workspace || workspace_bytes < sla_join_norm_backward_workspace_bytes(p, cu_seqlens != nullptr)))
-        return SLA_ERR_WORKSPACE;
+    const Split s = split(p->D, kBackwardWaves);
+    const unsigned blocks = backward_workgroups(s, tokens_of(*p, cu_seqlens != nullptr));
+    if (sums && (!workspace || workspace_bytes < sums_bytes(blocks, p->D))) return SLA_ERR_WORKSPACE;
     JoinArgs a{};
     a.x = x_out; a.h = h; a.w_after = w_after; a.channel = channel_scale; a.w_before = w_before; a.dy = dy; a.dxo = dx_out;
     a.dx = dx; a.dh = dh; a.part = sums ? (float*)workspace : nullptr;
     a.cu = cu_seqlens; a.tokens = tokens_of(*p, cu_seqlens); a.B = p->B; a.D = p->D;
     a.scale = p->scale; a.eps = p->eps; a.inv_d = 1.f / p->D;
-    const Split s = split(p->D, kBackwardWaves);
     a.row_waves = s.row_waves; a.rows = s.rows;
-    const unsigned blocks = backward_workgroups(s, a.tokens);
     const size_t lds = (2 * 16 * 4 + (size_t)(s.v == 1 ? s.rows - 1 : 1) * planes * s.row_waves * 64 * 8 * s.v) * sizeof(float);
 #define SLA_JN(X, Y, V)                                                                                                 \
     do {                                                                                                                \

@@ -188,15 +188,23 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_backward_kernel(GateAr
     }
 }
 
-int check_norm_gate(const sla_norm_gate_params* p, const void* g, const float* w, const int32_t* cu) {
+int64_t tokens_of(const sla_norm_gate_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
+
+// The sizes and types of a call or of a query for one.
+int check_sizes(const sla_norm_gate_params* p, bool packed) {
     if (!p) return SLA_ERR_NULL;
     if (p->dtype != SLA_F32 && p->dtype != SLA_BF16) return SLA_ERR_UNSUPPORTED;
     if (p->gate < kNone || p->gate > kSigmoid) return SLA_ERR_UNSUPPORTED;
     if (p->flags & ~(SLA_FLAG_HEAD_MAJOR | SLA_FLAG_HEAD_WEIGHTS)) return SLA_ERR_UNSUPPORTED;
-    if (cu && (p->flags & SLA_FLAG_HEAD_MAJOR)) return SLA_ERR_UNSUPPORTED;  // packed batches are [T,H,dv]
+    if (packed && (p->flags & SLA_FLAG_HEAD_MAJOR)) return SLA_ERR_UNSUPPORTED;  // packed batches are [T,H,dv]
     if (p->B < 0 || p->T < 0 || p->H < 1 || p->H > kMaxHeads) return SLA_ERR_SHAPE;
     if (p->dv < 8 || p->dv > kMaxWidth || (p->dv & 7) || !(p->eps >= 0.f)) return SLA_ERR_SHAPE;
-    if ((cu ? (int64_t)p->T : (int64_t)p->B * p->T) > (int64_t)1 << 30) return SLA_ERR_SHAPE;
+    return tokens_of(*p, packed) > (int64_t)1 << 30 ? SLA_ERR_SHAPE : SLA_OK;
+}
+
+int check_norm_gate(const sla_norm_gate_params* p, const void* g, const float* w, const int32_t* cu) {
+    const int rc = check_sizes(p, cu != nullptr);
+    if (rc != SLA_OK) return rc;
     if (p->B > 0 && p->T > 0 && (p->gate != kNone) != (g != nullptr)) return SLA_ERR_NULL;
     if ((p->flags & SLA_FLAG_HEAD_WEIGHTS) && !w) return SLA_ERR_NULL;
     if (!aligned(g, 16) || !aligned(w, 16) || !aligned(cu, 4)) return SLA_ERR_ALIGN;
@@ -226,7 +234,10 @@ unsigned workgroups(const GateArgs& a, int64_t tokens, int64_t most) {
 
 constexpr int64_t kBackwardGroups = kComputeUnits * 4;  // workgroups, and with them partial sums of dw
 
-int64_t tokens_of(const sla_norm_gate_params& p, bool packed) { return packed ? p.T : (int64_t)p.B * p.T; }
+// Bytes of the partial sums that so many workgroups of the backward leave.
+size_t sums_bytes(const GateArgs& a, unsigned blocks) {
+    return (a.per_head ? (size_t)(blocks / a.groups) * a.H : blocks) * (size_t)a.dv * sizeof(float);
+}
 
 }  // namespace
 
@@ -264,13 +275,11 @@ size_t sla_norm_gate_backward_workspace_bytes(const sla_norm_gate_params* p, int
     using namespace sla;
     if (!p) return 0;
     sla_norm_gate_params q = *p;
-    q.gate = kNone;
-    q.flags &= ~SLA_FLAG_HEAD_WEIGHTS;
-    if (check_norm_gate(&q, nullptr, nullptr, nullptr) != SLA_OK || p->B == 0 || p->T == 0) return 0;
+    q.gate = kNone;  // says nothing about the sums
+    if (check_sizes(&q, packed != 0) != SLA_OK || p->B == 0 || p->T == 0) return 0;
     GateArgs a{};
     layout(*p, a);
-    const size_t blocks = workgroups(a, tokens_of(*p, packed), kBackwardGroups);
-    return (a.per_head ? blocks / a.groups * a.H : blocks) * (size_t)a.dv * sizeof(float);
+    return sums_bytes(a, workgroups(a, tokens_of(*p, packed != 0), kBackwardGroups));
 }
 
 int sla_norm_gate_backward(const sla_norm_gate_params* p, const void* x, const void* g, const float* w, const void* dy,
@@ -289,11 +298,10 @@ int sla_norm_gate_backward(const sla_norm_gate_params* p, const void* x, const v
     layout(*p, a);
     const int width = a.per_head ? a.H * a.dv : a.dv;
     if (!work) return dw ? launch_column_sums(nullptr, 0, 1, width, dw, nullptr, nullptr, nullptr, nullptr, (hipStream_t)stream) : SLA_OK;
-    if (dw && (!workspace || workspace_bytes < sla_norm_gate_backward_workspace_bytes(p, cu_seqlens != nullptr)))
-        return SLA_ERR_WORKSPACE;
+    const unsigned blocks = workgroups(a, tokens_of(*p, cu_seqlens != nullptr), kBackwardGroups);
+    if (dw && (!workspace || workspace_bytes < sums_bytes(a, blocks))) return SLA_ERR_WORKSPACE;
     a.x = x; a.g = g; a.w = w; a.dy = dy; a.dx = dx; a.dg = dg; a.cu = cu_seqlens;
     a.part = dw ? (float*)workspace : nullptr;
-    const unsigned blocks = workgroups(a, tokens_of(*p, cu_seqlens), kBackwardGroups);
 #define SLA_NG(BF, G) \
     hipLaunchKernelGGL((sla_norm_gate_backward_kernel<BF, G>), dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, a)
     if (p->dtype == SLA_BF16) {
