@@ -931,12 +931,14 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-# Parameter blocks by value: a token's host time is part of every step, and building one costs a microsecond.
+# Parameter blocks by value: a token's host time is part of every step, and building one costs a microsecond.  Fields are Python
+# numbers: an object that holds one, such as a tensor, would be found again by its identity after its value has changed.
 @functools.lru_cache(maxsize=1024)
 def _params(kind, *fields):
     return ctypes.byref(kind(*fields))
 
 
+# The fields up to the scalars, which no size depends on.
 @functools.lru_cache(maxsize=1024)
 def _workspace_size(kind, *fields, packed):
     query = sla_norm_gate_backward_workspace_bytes if kind is SlaNormGateParams else sla_join_norm_backward_workspace_bytes
@@ -1061,7 +1063,7 @@ def _rotary(call, q, k, frequencies, start, positions, cu_seqlens, adjacent, mag
     if not fresh and k is not None and q.numel():
         _need(q_out.data_ptr() != k.data_ptr() and k_out.data_ptr() not in (q.data_ptr(), q_out.data_ptr()),
               "an output may lie on its own input only")
-    _run(call, q, _params(SlaRotaryParams, _element("q", el), B, T, Hq, Hk, d, 2 * pairs, flags, magnitude), q.data_ptr(),
+    _run(call, q, _params(SlaRotaryParams, _element("q", el), B, T, Hq, Hk, d, 2 * pairs, flags, float(magnitude)), q.data_ptr(),
          _ptr(k), frequencies.data_ptr(), _ptr(where), _ptr(cu_seqlens), q_out.data_ptr(), _ptr(k_out))
     return q_out, k_out
 
@@ -1103,7 +1105,7 @@ def _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major):
             _tensor("w", w, device, (H, dv), torch.float32)
         else:
             _tensor("w", w, device, (dv,), torch.float32)
-    return (SlaNormGateParams, _element("x", el), B, T, H, dv, kind, flags, eps), shape
+    return (SlaNormGateParams, _element("x", el), B, T, H, dv, kind, flags, float(eps)), shape
 
 
 def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None, head_major: bool = False, out=None):
@@ -1135,7 +1137,7 @@ def norm_gate_backward(x, g, w, dy, *, gate: str = "silu", eps: float = 1e-5, cu
     if workspace is not None:
         size = _workspace_bytes(workspace, x)
     elif dw is not None:
-        size = _workspace_size(*params, packed=cu_seqlens is not None)
+        size = _workspace_size(*params[:-1], packed=cu_seqlens is not None)
         workspace = x.new_empty(size, dtype=torch.uint8)
     _run(load_library().sla_norm_gate_backward, x, _params(*params), x.data_ptr(), _ptr(g), _ptr(w), dy.data_ptr(),
          _ptr(cu_seqlens), dx.data_ptr(), _ptr(dg), _ptr(dw), _ptr(workspace), size)
@@ -1171,7 +1173,7 @@ def _join_args(x, one, other, w_after, channel_scale, w_before, scale, eps, cu_s
         B, T = 1, x.numel() // D if D else 0
     if (T | D) >> 31:
         raise ValueError(f"x: {tuple(shape)} is out of range")
-    return SlaJoinNormParams, _element("h", kind), _element("x", el), B, T, D, scale, eps
+    return SlaJoinNormParams, _element("h", kind), _element("x", el), B, T, D, float(scale), float(eps)
 
 
 def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float = 1.0, eps: float = 1e-5, cu_seqlens=None,
@@ -1224,7 +1226,7 @@ def join_norm_backward(x_out, h, w_before, dy, dx_out=None, *, w_after=None, cha
         if workspace is not None:
             size = _workspace_bytes(workspace, x_out)
         elif dy is not None or dw_after is not None or dchannel is not None:
-            size = _workspace_size(*params, packed=cu_seqlens is not None)
+            size = _workspace_size(*params[:-2], packed=cu_seqlens is not None)
             workspace = x_out.new_empty(size, dtype=torch.uint8)
         _run(load_library().sla_join_norm_backward, x_out, _params(*params), x_out.data_ptr(), _ptr(h), _ptr(w_after),
              _ptr(channel_scale), _ptr(w_before), _ptr(dy), _ptr(dx_out), _ptr(cu_seqlens), None if dy is None else dx.data_ptr(),
