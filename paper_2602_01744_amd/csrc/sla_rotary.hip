@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void sla_rotary_kernel(RotaryArgs a) {
             t = n - b * a.T;
         } else if (!a.per_token) {
             b = sequence_of(a.cu, a.B, n);
-            t = n - a.cu[b];
+            t = n - (a.cu[b] > 0 ? a.cu[b] : 0);  // a start in front of the tensors is their first token
         }
         double pos;
         if (a.per_token)
