@@ -58,7 +58,7 @@ __device__ __forceinline__ void turn(double t, float m, float sign, float& c, fl
 __device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int64_t n) {
     int lo = 0, hi = B;  // cu[lo] <= n < cu[hi]
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
+        const int mid = lo + ((hi - lo) >> 1);  // the sum of two ends may pass 2^31
         if (cu[mid] <= n) lo = mid; else hi = mid;
     }
     return lo;

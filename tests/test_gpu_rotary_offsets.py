@@ -43,3 +43,22 @@ def test_positions_count_from_the_clamped_start(dtype, adjacent, r, cu):
             pair = np.abs(x[inside][..., a].astype(np.float64)) + np.abs(x[inside][..., b])
             terms[..., a] = terms[..., b] = (8 + 2.0 ** -41 / STEP) * pair
             within(name, got[inside], want, terms, dtype, steps=1)
+
+
+def test_more_than_2_30_sequences():
+    """The search for a token's sequence halves ranges whose ends add to more than 2^31; all sequences but two are empty."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    B, T = (1 << 30) + 5, 9
+    if torch.cuda.mem_get_info()[0] < 12 * 2 ** 30:
+        pytest.skip("not enough memory")
+    cu = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    start = torch.zeros(B, dtype=torch.int32, device="cuda")
+    cu[-2], cu[-1], start[-2], start[-1] = 4, T, 70, 100000
+    x = torch.randn(T, 2, 64, device="cuda")
+    f, _ = sla.rotary_frequencies(64)
+    y, _ = sla.rotary(x, None, f, cu_seqlens=cu, start=start)
+    at = torch.tensor([70, 71, 72, 73, 100000, 100001, 100002, 100003, 100004], dtype=torch.int32, device="cuda")
+    want, _ = sla.rotary(x[None], None, f, positions=at[None])
+    assert torch.equal(y, want[0])
