@@ -147,10 +147,17 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_backward_kernel(GateAr
         for (int i = 0; i < 8; ++i) {
             float act = 1.f;
             if (GATE != kNone) {
-                const float q = sigmoid(g[i]);
-                act = GATE == kSilu ? g[i] * q : q;
                 // g becomes the gate's derivative
-                g[i] = GATE == kSilu ? q * (1.f + g[i] * (1.f - q)) : q * (1.f - q);
+                if (GATE == kSilu) {
+                    const float q = sigmoid(g[i]);
+                    act = g[i] * q;
+                    g[i] = q * (1.f + g[i] * (1.f - q));
+                } else {  // e^-|g| / (1 + e^-|g|)^2: the difference 1 - q would lose an open gate's slope
+                    const float e = __builtin_amdgcn_exp2f(-fabsf(g[i]) * lane_ops::kLog2e);
+                    const float near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
+                    act = g[i] < 0.f ? far : near;
+                    g[i] = near * far;
+                }
             }
             dn[i] = dy[i] * act;  // the weight comes later: the sum for dw takes it without
             s += x[i] * x[i];
