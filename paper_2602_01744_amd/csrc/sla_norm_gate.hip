@@ -39,8 +39,18 @@ struct GateArgs {
     float eps, inv_dv;
 };
 
+// exp(-g).  The product with log2 e is rounded, by up to |g| 2^-24 of the result: with EXACT what it lost comes back as a factor
+// (not where the result leaves the normal range).  A gate in bf16 needs none of it: at most 2^-17 there, half a step is 2^-9.
+template <bool EXACT>
+__device__ __forceinline__ float exp_minus(float g) {
+    const float t = -g * lane_ops::kLog2e, e = __builtin_amdgcn_exp2f(t);
+    if (!EXACT) return e;
+    const float lost = __builtin_fmaf(g, -1.92596299e-8f, __builtin_fmaf(g, -lane_ops::kLog2e, -t));  // log2 e = kLog2e + 1.926e-8
+    return fabsf(t) < 126.f ? __builtin_fmaf(e * 0.693147181f, lost, e) : e;
+}
+template <bool EXACT>
 __device__ __forceinline__ float sigmoid(float g) {
-    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-g * lane_ops::kLog2e));
+    return __builtin_amdgcn_rcpf(1.f + exp_minus<EXACT>(g));
 }
 
 // Where a lane works: head h, piece e of it, tokens first + its slot, then every `step`-th.
@@ -108,8 +118,8 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_kernel(GateArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float v = x[u][i] * r * w[i];
-                if (GATE == kSilu) v *= g[u][i] * sigmoid(g[u][i]);
-                if (GATE == kSigmoid) v *= sigmoid(g[u][i]);
+                if (GATE == kSilu) v *= g[u][i] * sigmoid<!BF16>(g[u][i]);
+                if (GATE == kSigmoid) v *= sigmoid<!BF16>(g[u][i]);
                 x[u][i] = v;
             }
             if (p.live && n < p.end) store8<BF16>(a.y, offset_y(a, p, n), x[u]);
@@ -149,11 +159,11 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_backward_kernel(GateAr
             if (GATE != kNone) {
                 // g becomes the gate's derivative
                 if (GATE == kSilu) {
-                    const float q = sigmoid(g[i]);
+                    const float q = sigmoid<!BF16>(g[i]);
                     act = g[i] * q;
                     g[i] = q * (1.f + g[i] * (1.f - q));
                 } else {  // e^-|g| / (1 + e^-|g|)^2: the difference 1 - q would lose an open gate's slope
-                    const float e = __builtin_amdgcn_exp2f(-fabsf(g[i]) * lane_ops::kLog2e);
+                    const float e = exp_minus<!BF16>(fabsf(g[i]));
                     const float near = __builtin_amdgcn_rcpf(1.f + e), far = e * near;
                     act = g[i] < 0.f ? far : near;
                     g[i] = near * far;

@@ -41,3 +41,41 @@ def test_slopes_of_open_and_closed_gates(dtype, kind):
     t = np.abs(dy * nw)
     # K for the norm, 2 |g| for the exponential
     within("dg", dg, dy * nw * slope, t * terms * (1 + 2 * np.abs(g) / K), dtype)
+
+
+@pytest.mark.parametrize("kind", ["sigmoid", "silu"])
+def test_exponentials_of_far_gates_in_fp32(kind):
+    """The exponential's error does not grow with |g|.  Rows of ones and eps = 0 make the norm exact, so what is left is the gate's:
+    2 steps each for exp2 and the reciprocal, one each for the exponent's correction, 1 + e and every product; 12 in all.  SiLU's
+    slope forms 1 - p from p, whose 4 steps |g| multiplies while the gate is not yet open (p < 1, g < 18)."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    g = np.linspace(-86, 86, 64 * 256).astype(np.float32).reshape(1, 64, 4, 64)
+    gt = tensor(g)
+    one = torch.ones_like(gt)
+    y = sla.norm_gate(one, gt, None, gate=kind, eps=0.0)
+    dg = sla.norm_gate_backward(one, gt, None, one, gate=kind, eps=0.0)["dg"]
+    act, slope, terms = _gate(g.astype(np.float64), kind)
+    within("y", y, act, np.abs(act), "f32", steps=12)
+    more = 4 * np.clip(g, 0, 18) if kind == "silu" else 0
+    within("dg", dg, slope, terms * (16 + more), "f32", steps=1)
+
+
+def test_infinite_gates():
+    """The limits where they exist: closed and open sigmoids, an open SiLU; NaN stays in its place."""
+    import torch
+    import paper_2602_01744_amd as sla
+
+    inf = float("inf")
+    for dtype in (torch.float32, torch.bfloat16):
+        g = torch.tensor([inf, -inf, float("nan"), 3e38, -3e38, 0.0, 90.0, -90.0], device="cuda").repeat(8).view(1, 1, 1, 64).to(dtype).contiguous()
+        one = torch.ones_like(g)
+        y = sla.norm_gate(one, g, None, gate="sigmoid", eps=0.0)[0, 0, 0, :8].float().tolist()
+        assert y[:2] == [1.0, 0.0] and np.isnan(y[2]) and y[3:7] == [1.0, 0.0, 0.5, 1.0] and 0 <= y[7] < 1e-38
+        d = sla.norm_gate_backward(one, g, None, one, gate="sigmoid", eps=0.0)["dg"][0, 0, 0, :8].float().tolist()
+        assert d[:2] == [0.0, 0.0] and np.isnan(d[2]) and d[3:6] == [0.0, 0.0, 0.25] and max(d[6:]) < 1e-38
+        y = sla.norm_gate(one, g, None, gate="silu", eps=0.0)[0, 0, 0, :8].float().tolist()
+        assert y[0] == inf and np.isnan(y[2]) and y[3] == float(g[0, 0, 0, 3]) and y[4] == 0 and y[5:7] == [0.0, 90.0]
+        d = sla.norm_gate_backward(one, g, None, one, gate="silu", eps=0.0)["dg"][0, 0, 0, :8].float().tolist()
+        assert np.isnan(d[2]) and d[3:6] == [1.0, 0.0, 0.5] and d[6] == 1.0 and abs(d[7]) < 1e-36
