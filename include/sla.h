@@ -457,8 +457,9 @@ int sla_rotary_backward(const sla_rotary_params* p, const void* dq_out, const vo
  *            that share it) in a fixed order; zeros for an empty batch
  *   workspace  sla_norm_gate_backward_workspace_bytes(p, packed) bytes, 16-byte aligned, for dw (packed: with cu_seqlens);
  *            contents undefined before and after, calls that share it must not overlap
- * y may be g or, without SLA_FLAG_HEAD_MAJOR, x (the same address); nothing else may overlap.  Sums of squares are fp32: a
- * vector with a value over 1e19 is divided by infinity.
+ * y may be g or, without SLA_FLAG_HEAD_MAJOR, x (the same address); nothing else may overlap.  Squares and their sums are fp32:
+ * a vector with a value over 1e19 is divided by infinity; with eps = 0 one whose values are all under 1e-19 loses digits (its mean
+ * square is off by up to 2^-149), and under 1e-23 it counts as zeros, 0 / 0.
  */
 typedef enum { SLA_GATE_NONE = 0, SLA_GATE_SILU = 1, SLA_GATE_SIGMOID = 2 } sla_gate;
 #define SLA_FLAG_HEAD_WEIGHTS 2
@@ -481,7 +482,8 @@ size_t sla_norm_gate_backward_workspace_bytes(const sla_norm_gate_params* p, int
 /*
  * The join of a block's output h with the residual stream x, and the norm in front of the next block:
  *     u = h, or with w_after h / sqrt(mean(h^2) + eps) * w_after;   x' = x + scale * c * u;   y = x' / sqrt(mean(x'^2) + eps) * w_before
- * (c = channel_scale, or 1; means over the width D; x' enters y before it is rounded to the stream's type).
+ * (c = channel_scale, or 1; means over the width D, with the limits of the read-out's; x' enters y before it is rounded to the
+ * stream's type).
  *
  *   x, x_out, dx, dx_out   [B,T,D]  x_dtype   the stream
  *   h, y, dh, dy           [B,T,D]  dtype

@@ -90,9 +90,11 @@ __device__ __forceinline__ float lanes_sum(float s, int lanes) {
     return s;
 }
 
-// 1 / sqrt(x): the hardware's, within one unit of the last place, and a Newton step; 0 and infinity keep the hardware's.
+// 1 / sqrt(x): the hardware's, within one unit of the last place, and a Newton step; 0 and infinity keep the hardware's.  Values
+// under the normal range, which the instruction takes for 0, are scaled into it first.
 __device__ __forceinline__ float inverse_root(float x) {
-    const float y = __builtin_amdgcn_rsqf(x);
+    const bool tiny = x < 0x1p-126f;
+    const float y = __builtin_amdgcn_rsqf(tiny ? x * 0x1p64f : x) * (tiny ? 0x1p32f : 1.f);
     const float z = __builtin_fmaf(0.5f * y, __builtin_fmaf(-x * y, y, 1.f), y);
     return y > 0.f && y < INFINITY ? z : y;
 }
