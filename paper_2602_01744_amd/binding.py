@@ -1181,12 +1181,15 @@ def join_norm(x, h, w_before, *, w_after=None, channel_scale=None, scale: float 
     """A block's output h joins the residual stream x, and the stream is normalised for the next block (sla_join_norm):
     u = h, or h / rms(h) * w_after;  x_out = x + scale * channel_scale * u;  y = x_out / rms(x_out) * w_before.  x, h [..., D]
     ([T,D] with cu_seqlens), x float32 or of h's type; weights float32 [D].  Returns (x_out, y).  h None: no join, x_out is x, and
-    y has y_dtype (default: x's type); w_before None: no norm, y is None.  ``x_out`` may be x and ``y`` may be h."""
+    y has y_dtype (default: y's type if it is given, else x's); w_before None: no norm, y is None.  ``x_out`` may be x and ``y`` may be h."""
     torch = sys.modules["torch"]
     if h is None:
         _need(w_before is not None and w_after is None and channel_scale is None and x_out is None,
               "h: needed, unless only the norm of x is asked for")
     _need(w_before is not None or y is None, "an output y, but no w_before")
+    if y_dtype is not None and w_before is not None:
+        like = h if h is not None else y
+        _need(like is None or like.dtype is y_dtype, "y_dtype: y has the type of h, or of the tensor given for it")
     params = _join_args(x, h, y, w_after, channel_scale, w_before, scale, eps, cu_seqlens, y_dtype)
     if y is not None and x.numel():
         _need(y.data_ptr() not in (x.data_ptr(), _ptr(x_out)), "y may lie on h only")
