@@ -274,10 +274,13 @@ int sla_norm_gate(const sla_norm_gate_params* p, const void* x, const void* g, c
     GateArgs a{};
     layout(*p, a);
     a.x = x; a.g = g; a.w = w; a.y = y; a.cu = cu_seqlens;
-    // Rows that lie apart in x want fewer workgroups that walk on: bf16, B=8 T=2048 16 heads of 128, head-major, with 4, 8, 32 and
-    // 64 a compute unit 36.8, 37.5, 41.9, 43.6 us, B=8 T=4096 4 heads of 256 36.9, 39.6, 44.0 us; token-major, T=65536 16 heads of
-    // 128, 151 us with 8 and 142 with 64.
-    const dim3 grid(workgroups(a, tokens_of(*p, cu_seqlens), kComputeUnits * (a.head_major ? 4 : 64)));
+    // bf16 rows that lie apart in x want fewer workgroups that walk on: head-major, with 4, 8, 16 and 64 a compute unit, B=8 T=2048 16
+    // heads of 128 37.0, 37.9, 38.0, 46 us, B=8 T=4096 4 heads of 256 37.4, 39.5, 40.1, 44, 8 of 64 18.9, 19.3, 21.8, 21.3, 2 of 512
+    // 36.1, 40.0, 39.5, 44, B=16384 T=1 16 of 128 35.1, 35.6, 37.6, 43; only a single long row differs, T=65536 149, 154, 160, 143.
+    // fp32 rows are twice as long and want what token-major ones do: with 4, 16 and 64, B=4 T=2048 16 of 128 38.2, 35.3, 34.1 us, B=8
+    // T=2048 8 of 128 36.5, 35.0, 33.3, B=8 T=4096 2 of 256 35.8, 35.5, 34.1, B=4 T=2048 32 of 64 37.0, 36.3, 35.3; only B=4 T=4096 4 of
+    // 256 differs, 35.3, 37.6, 37.5.  Token-major bf16, T=65536 16 heads of 128: 151 us with 8 and 142 with 64.
+    const dim3 grid(workgroups(a, tokens_of(*p, cu_seqlens), kComputeUnits * (a.head_major && p->dtype == SLA_BF16 ? 4 : 64)));
 #define SLA_NG(BF, G) hipLaunchKernelGGL((sla_norm_gate_kernel<BF, G>), grid, dim3(kThreads), 0, (hipStream_t)stream, a)
     if (p->dtype == SLA_BF16) {
         if (p->gate == kNone) SLA_NG(true, kNone); else if (p->gate == kSilu) SLA_NG(true, kSilu); else SLA_NG(true, kSigmoid);
