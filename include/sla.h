@@ -448,6 +448,9 @@ int sla_rotary_backward(const sla_rotary_params* p, const void* dq_out, const vo
 /*
  * The read-out: every head's output of the mixer divided by its root mean square, weighted and gated,
  *     n = x / sqrt(mean(x^2) + eps),   y = n w act(g)           act(g) = g sigmoid(g), sigmoid(g), or 1
+ * It is the read-out of the base models' blocks.  A norm over each head divides out what multiplies the head's whole vector, and
+ * the read gate G^Q (Eq. 4) does: where (G^Q)^2 mean(o^2) is large against eps, y does not depend on G^Q and its logits have no
+ * gradient.  A layer that is to keep it normalises over all heads of a token (sla_join_norm with h NULL, D = H dv), or not at all.
  * and its gradients from the same inputs and the cotangent dy of y (nothing is kept from the forward call):
  *
  *   x, dx    [B,T,H,dv]  dtype   with SLA_FLAG_HEAD_MAJOR [B,H,T,dv], as sla_forward leaves out there; rectangular batches only

@@ -1112,7 +1112,8 @@ def norm_gate(x, g, w, *, gate: str = "silu", eps: float = 1e-5, cu_seqlens=None
     """The read-out behind the mixer: y = x / sqrt(mean(x^2) + eps) * w * act(g) over every head vector (sla_norm_gate).
     x, g [B,T,H,dv] ([T,H,dv] with cu_seqlens, [B,H,dv] for one token each), w float32 [dv], [H,dv] or None; gate "silu",
     "sigmoid" or "none" (then g is None).  head_major: x is [B,H,T,dv], g and y are [B,T,H,dv].  ``out`` may be g or, without
-    head_major, x."""
+    head_major, x.  A norm over each head divides out the mixer's read gate, which scales the head's whole vector; ``join_norm`` of
+    x.view(B, T, H * dv) with h None normalises over all heads and keeps it."""
     params, shape = _norm_gate_args(x, g, w, eps, gate, cu_seqlens, head_major)
     if out is None:
         out = x.new_empty(shape) if head_major else sys.modules["torch"].empty_like(x)
