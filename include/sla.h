@@ -418,7 +418,8 @@ size_t sla_gate_logits_backward_workspace_bytes(const sla_params* p);
  * th = position * frequency and scaled:
  *     a' = m (a cos th - b sin th),   b' = m (a sin th + b cos th);      elements from `rotary` on are copied.
  * Pair i is elements (i, i + rotary/2), or with SLA_FLAG_ADJACENT_PAIRS (2i, 2i+1).  The angles are formed in the kernel, in
- * 64 bits, so that they lose nothing far into a context (|position * frequency| up to 2^31).
+ * 64 bits, for |position * frequency| up to 2^31: each is off by at most |position * frequency| 2^-51 radians, which stays under
+ * fp32's 2^-24 up to 2^27 radians.
  *
  *   q, q_out         [B,T,Hq,d]  dtype   ([B,Hq,T,d] with SLA_FLAG_HEAD_MAJOR, rectangular batches only)
  *   k, k_out         [B,T,Hk,d]  dtype   NULL with Hk == 0

@@ -9,9 +9,10 @@
 // last-level cache holds part of it): B=8 T=2048 16+16 heads of 128, 268 MB, 45 us; T=65536 32+32 heads, 2.1 GB, 378 us.
 //
 // The angles are made here instead of read from a table: a lane forms one to four of a token's, and every head of the token
-// that the wave walks takes them.  An angle is reduced to a quarter turn in fp64 (position * frequency / 2 pi minus its
-// nearest multiple of 1/4: exact but for the product's rounding of 2^-53), so far positions cost no accuracy; sine and cosine
-// of what is left, |x| <= pi/4, are their Taylor polynomials.
+// that the wave walks takes them.  An angle is reduced to a quarter turn in fp64: position * frequency / 2 pi minus its
+// nearest multiple of 1/4, a difference that is exact; 1 / 2 pi and the two products are rounded by 2^-53 each, so the angle is off
+// by less than 2^-51 of itself, under fp32's 2^-24 up to 2^27 radians.  Sine and cosine of what is left, |x| <= pi/4, are their
+// Taylor polynomials of degree 9 and 10, off by less than 2.5e-9 and 2e-10 of them.
 #include "sla_row_ops.h"
 
 namespace sla {
