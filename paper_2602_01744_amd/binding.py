@@ -863,6 +863,9 @@ def forward(
 
 # ---------------------------------------------------------------------------------------------------------------------
 # Around the mixer: rotary positions, the normalised and gated read-out, the join with the residual stream.
+#
+# Scalars (magnitude, eps, scale) are numbers; where a tensor holds one, its value is read on the host at every call.  With cu_seqlens,
+# rows outside every sequence stay as they were in an output that is passed and are undefined in a new one.
 
 def sla_rotary(params, q, k, frequencies, positions, cu_seqlens, q_out, k_out, stream) -> int:
     """Raw call: integer device addresses (0/None = NULL) and a hipStream_t handle.  Returns the status code."""

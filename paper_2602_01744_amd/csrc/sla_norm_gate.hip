@@ -41,7 +41,7 @@ struct GateArgs {
 
 // p = 1 / (1 + exp(-g)) and rest = 1 - p, which a difference would lose where the gate is open: both from e = exp(-|g|).  In fp32
 // (EXACT) what the product |g| log2 e loses to rounding, up to |g| 2^-24 of e, comes back as a factor (not where e leaves the normal
-// range), and the reciprocal has a Newton step: 4 steps of 2^-24 in all.  bf16 needs neither: at most 2^-17, half a step is 2^-9.
+// range), and the reciprocal has a Newton step: 5 steps of 2^-24 in all.  bf16 needs neither: at most 2^-17, half a step is 2^-9.
 template <bool EXACT>
 __device__ __forceinline__ float sigmoid(float g, float& rest) {
     const float m = fabsf(g), t = -m * lane_ops::kLog2e;

@@ -83,6 +83,10 @@ def test_packed_host_code_under_sanitizers(tmp_path):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     if not (os.path.exists(hipcc) or shutil.which(hipcc)):
         pytest.skip("hipcc not available")
+    import torch
+
+    if torch.cuda.is_available():
+        pytest.skip("valid calls end at their launch only where there is no GPU")
     exe = str(tmp_path / "layer_packed_san")
     host = [x for f in ("address", "undefined") for x in ("-Xarch_host", f"-fsanitize={f}")] + ["-Xarch_host", "-fno-sanitize-recover=all"]
     csrc = os.path.join(ROOT, "paper_2602_01744_amd", "csrc")
