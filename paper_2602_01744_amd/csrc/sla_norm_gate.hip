@@ -9,8 +9,8 @@
 // T=4096 16 heads of 128, 671 MB, 131 to 136 us.  A head's vector lies in dv/8 lanes (a power of
 // two of them is set aside), eight elements each, so its sums are a few lane exchanges and nothing is read twice.  A wave
 // covers as many heads of a token as divide H, then several tokens: a lane keeps to one head, whose weights stay in
-// registers.  dw is summed in two stages in a fixed order: over a workgroup's tokens in registers and LDS, then, in 64 bits, over
-// the workgroups' partial sums; no atomics, so results do not change from run to run.
+// registers.  dw is summed in a fixed order: a lane's tokens in fp32 registers, then, in 64 bits, the lanes of a workgroup through
+// LDS and, in a second kernel, the workgroups' partial sums (fp32 in memory); no atomics, so results do not change from run to run.
 #include "sla_row_ops.h"
 
 namespace sla {
@@ -202,8 +202,9 @@ __global__ __launch_bounds__(kThreads) void sla_norm_gate_backward_kernel(GateAr
     const int heads = a.per_head ? a.wave_heads : 1, slots = kThreads / a.lanes;
     for (int j = threadIdx.x; j < heads * a.dv; j += kThreads) {
         const int hh = j / a.dv, col = j - hh * a.dv;
-        float s = 0.f;
-        for (int q = hh; q < slots; q += heads) s += red[(q * a.lanes + col / 8) * 8 + col % 8];
+        double sum = 0.0;  // up to 256 slots one after the other
+        for (int q = hh; q < slots; q += heads) sum += red[(q * a.lanes + col / 8) * 8 + col % 8];
+        const float s = (float)sum;
         const size_t blk = blockIdx.x / a.groups, grp = blockIdx.x % a.groups;
         if (a.per_head)
             a.part[(blk * a.H + grp * heads + hh) * a.dv + col] = s;
